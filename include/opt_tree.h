@@ -251,6 +251,100 @@ int opt_tree_step_host(opt_tree_ctx *ctx, const void *draft_logits_bf16, const v
                        const int32_t *root_token_host, const int32_t *base_pos_host, int32_t B, float delta,
                        const opt_tree_host_out *out, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------------
+ * Attention layers of the target model around a tree step: a paged 8-bit key/value cache, the attention that reads it with the
+ * tree's mask, and the move of the accepted entries.  The paper keeps key and value caches in both models (Section 3) and hands
+ * the tree's mask to the target's attention (Algorithm 2) but fixes no formats; this library's are:
+ *
+ *   cache    k, v (dev) [layers][num_pages][kv_heads][page][head_dim] e4m3 codes, 16-byte aligned, and
+ *            k_scale, v_scale (dev) [layers][num_pages][kv_heads] float: an entry stands for code * scale.  opt_tree_kv_append and
+ *            opt_tree_kv_compact write powers of two; opt_tree_kv_attend takes any positive finite scale.
+ *            block_table (dev) [B][max_pages] int32: slot s of sequence b (its s-th cached token) is row s % page of page
+ *            block_table[b][s / page].  Entries beyond a sequence's last slot are not read.  Sequences may share pages that lie wholly below
+ *            their kv_len; a page that takes a step's tokens belongs to one sequence and stands once in its table.
+ *   step     the step's tokens of sequence b: T = n + 1 positions, 0 the root, i + 1 packed node i (as opt_tree_post_verify);
+ *            kv_len (dev) [B]            slots cached before the step; the step's token j is slot kv_len + j
+ *            nodes (dev) [B] or NULL     nodes of the step (opt_tree_out's n_sel), nodes + 1 tokens; NULL: T - 1; negative: the
+ *                                        sequence takes no part in the step
+ *            base_pos (dev) [B] or NULL  position of the root (as opt_tree_mask); NULL: kv_len
+ *            position_ids (dev) [B][T-1] or NULL   positions of the nodes (as written by opt_tree_mask); NULL: base + 1, base + 2, ...
+ *            mask (dev) [B][T-1][ceil((T-1)/64)] or NULL   as written by opt_tree_mask: bit j of row i lets node i see node j.  Every
+ *                                        token sees the whole prefix, the root and itself.  NULL: a chain, every token sees the
+ *                                        tokens before it (T = 1: plain decoding; a prompt's chunk)
+ *   rows     q, k, v and outputs: 16-bit elements (dtype of the handle) [B][T][heads][head_dim], strides in elements, head_dim
+ *            contiguous; any base a 16-bit element may have, fastest where base and strides are multiples of 16 bytes.
+ * Tokens beyond a sequence's nodes + 1 are padding: neither read nor written anywhere.
+ *
+ * A handle owns a workspace and a status word only and belongs to the device that was current at its creation; calls are made
+ * with that device current (otherwise OPT_TREE_ERR_INVALID_ARG).  The calls only enqueue work on `stream`, may be captured into
+ * graphs, and never allocate or synchronise.  Calls on one handle share its workspace: those that may run at the same time (two
+ * streams, two graphs) need a handle each.  Sizes that only the device knows are checked there: a sequence whose kv_len or nodes do not fit,
+ * a page or a position that does not exist is recorded as OPT_TREE_ERR_INTERNAL in the status word; such a sequence (for a single page or
+ * position: what hangs on it) has unspecified results, and nothing out of bounds is touched. */
+typedef struct opt_tree_kv opt_tree_kv;
+
+#define OPT_TREE_BF16 0
+#define OPT_TREE_FP16 1
+
+/*   q_heads, kv_heads   q_heads a multiple of kv_heads; query head h reads key head h / (q_heads / kv_heads)
+ *   head_dim            64 or 128
+ *   page                tokens of a page: 16, 32, 64 or 128
+ *   num_pages           pages of the cache;  max_pages: pages of a sequence (width of the block table)
+ *   max_batch, max_step largest B and T any call will pass
+ *   layers              layers of the cache
+ *   dtype               OPT_TREE_BF16 or OPT_TREE_FP16: type of q, k, v, norm weights and outputs */
+typedef struct {
+    int32_t q_heads, kv_heads, head_dim, page, num_pages, max_pages, max_batch, max_step, layers, dtype;
+} opt_tree_kv_config;
+
+typedef struct { uint8_t *k, *v; float *k_scale, *v_scale; const int32_t *block_table; } opt_tree_kv_cache;
+typedef struct { int32_t B, T; const int32_t *kv_len, *nodes, *base_pos, *position_ids; const uint64_t *mask; } opt_tree_kv_step;
+typedef struct { const void *data; int64_t batch, token, head; } opt_tree_kv_rows;      /* strides in elements */
+
+/* What is done to queries and keys before they are used, in this order (zeros: nothing):
+ *   q_norm, k_norm      (dev) [head_dim] or NULL: x * rsqrt(mean(x^2) + eps) * weight, per token and head
+ *   cos_sin             (dev) [positions][rot_dim] float: rot_dim/2 cosines, then rot_dim/2 sines, of each position.  The first rot_dim
+ *                       elements (a multiple of 16; 0: no rotation) are rotated in pairs (i, i + rot_dim/2), or (2i, 2i + 1) if
+ *                       interleaved */
+typedef struct {
+    const float *cos_sin; int32_t positions, rot_dim, interleaved;
+    const void *q_norm, *k_norm; float eps;
+} opt_tree_kv_turn;
+
+size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config *cfg);       /* 0 if cfg is invalid or unsupported */
+int opt_tree_kv_create(opt_tree_kv **kv, const opt_tree_kv_config *cfg);
+int opt_tree_kv_destroy(opt_tree_kv *kv);
+
+/* Norm and rotation of the step's queries and keys, and the step's keys and values into layer `layer` of the cache.
+ *   q, q_out   rows of q_heads, or both NULL; q_out may be q itself.  k, v: rows of kv_heads
+ * Per page and head the scale becomes s = max(s_old, 2^max(-64, ceil(log2(a / 448)))) with a the largest magnitude of the step's entries
+ * in it and s_old the page's scale if it holds older slots (below kv_len), else 0; older entries are brought to s (exactly, but
+ * for those that become subnormal) and the new ones are e4m3(x / s), rounded to nearest even from single precision.  Infinite
+ * inputs saturate and NaN stays NaN; neither sets the scale.  The page's rows behind the step's last are left as they were.
+ * Norm and rotation are computed in single precision and q_out is rounded once; the scale is that of exact arithmetic. */
+int opt_tree_kv_append(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t layer, const opt_tree_kv_rows *q, const opt_tree_kv_rows *k,
+                       const opt_tree_kv_rows *v, const opt_tree_kv_rows *q_out, const opt_tree_kv_step *step, const opt_tree_kv_turn *turn,
+                       void *stream);
+
+/* out_i = sum_j softmax_j(scale * q_i . k_j) v_j over the slots that token i of the step sees, whose keys and values are in layer `layer`
+ * of the cache (the step's own included: append first).
+ *   q, out     rows of q_heads (q as opt_tree_kv_append wrote it); scale > 0, usually head_dim^-0.5
+ *   lse        (dev) [B][T][q_heads] float or NULL: log of the sum of exp(scale * q_i . k_j) */
+int opt_tree_kv_attend(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t layer, const opt_tree_kv_rows *q, const opt_tree_kv_step *step,
+                       float scale, const opt_tree_kv_rows *out, float *lse, void *stream);
+
+/* The accepted path's entries of all layers to the end of the prefix: slot kv_len + kv_gather[j] -> slot kv_len + j, j < kv_keep.
+ *   kv_gather  (dev) [B][G], kv_keep (dev) [B]: as written by opt_tree_post_verify (G = max_depth + 1 <= 1024); strictly ascending
+ *   new_len    (dev) [B] or NULL, not kv_len itself: kv_len + kv_keep, the next step's kv_len
+ * A page that takes entries whose scale is larger than its own is brought to the largest of them, all its rows.  A sequence with
+ * entries out of order or out of range is left as it is (new_len = kv_len, OPT_TREE_ERR_INTERNAL in the status word); kv_keep 0: nothing moves. */
+int opt_tree_kv_compact(opt_tree_kv *kv, const opt_tree_kv_cache *cache, const int32_t *kv_len, const int32_t *kv_gather,
+                        const int32_t *kv_keep, int32_t G, int32_t B, int32_t *new_len, void *stream);
+
+/* As opt_tree_last_device_status and opt_tree_launch_count, for the handle. */
+int opt_tree_kv_last_device_status(opt_tree_kv *kv, int32_t *status_host);
+int64_t opt_tree_kv_launch_count(const opt_tree_kv *kv);
+
 /* Self-test of the library's bounded device-side waits (not a step of the paper's method; the
  * persistent build waits on mailboxes, counters and shared-memory barriers, each wait with a limit
  * after which it records OPT_TREE_ERR_TIMEOUT and returns instead of hanging).  Launches one small

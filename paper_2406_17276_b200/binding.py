@@ -20,7 +20,9 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_TIMEOUT, ERR_INTERNAL = 0, -
 EXPORTS = ["opt_tree_workspace_bytes", "opt_tree_create", "opt_tree_destroy", "opt_tree_build", "opt_tree_mask",
            "opt_tree_verify", "opt_tree_row_softmax_topk", "opt_tree_step_host", "opt_tree_last_device_status",
            "opt_tree_launch_count", "opt_tree_strerror", "opt_tree_verify_static", "opt_tree_post_verify", "opt_tree_build_pruned", "opt_tree_layers_begin",
-           "opt_tree_layers_step", "opt_tree_verify_sampled", "opt_tree_selftest_waits", "opt_tree_selftest_selection"]
+           "opt_tree_layers_step", "opt_tree_verify_sampled", "opt_tree_selftest_waits", "opt_tree_selftest_selection",
+           "opt_tree_kv_workspace_bytes", "opt_tree_kv_create", "opt_tree_kv_destroy", "opt_tree_kv_append", "opt_tree_kv_attend",
+           "opt_tree_kv_compact", "opt_tree_kv_last_device_status", "opt_tree_kv_launch_count"]
 
 
 class Config(C.Structure):
@@ -36,6 +38,28 @@ class HostOut(C.Structure):
     _fields_ = [(f, C.c_void_p) for f in
                 ("token", "parent", "depth", "phat", "n_sel", "depth_reached", "expected_len", "mask", "position_ids",
                  "accept_len", "accept_tokens", "accept_nodes", "next_root")]
+
+
+class KVConfig(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("q_heads", "kv_heads", "head_dim", "page", "num_pages", "max_pages", "max_batch", "max_step",
+                                         "layers", "dtype")]
+
+
+class KVCacheC(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("k", "v", "k_scale", "v_scale", "block_table")]
+
+
+class KVStepC(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32)] + [(f, C.c_void_p) for f in ("kv_len", "nodes", "base_pos", "position_ids", "mask")]
+
+
+class KVRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class KVTurn(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("positions", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float)]
 
 
 _lib = None
@@ -77,6 +101,17 @@ def lib():
                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.opt_tree_selftest_waits.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
         L.opt_tree_selftest_selection.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32] + [C.c_void_p] * 5
+        L.opt_tree_kv_workspace_bytes.restype = C.c_size_t
+        L.opt_tree_kv_workspace_bytes.argtypes = [C.POINTER(KVConfig)]
+        L.opt_tree_kv_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(KVConfig)]
+        L.opt_tree_kv_destroy.argtypes = [C.c_void_p]
+        rows, cache, step = C.POINTER(KVRows), C.POINTER(KVCacheC), C.POINTER(KVStepC)
+        L.opt_tree_kv_append.argtypes = [C.c_void_p, cache, C.c_int32, rows, rows, rows, rows, step, C.POINTER(KVTurn), C.c_void_p]
+        L.opt_tree_kv_attend.argtypes = [C.c_void_p, cache, C.c_int32, rows, step, C.c_float, rows, C.c_void_p, C.c_void_p]
+        L.opt_tree_kv_compact.argtypes = [C.c_void_p, cache, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+        L.opt_tree_kv_last_device_status.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
+        L.opt_tree_kv_launch_count.restype = C.c_int64
+        L.opt_tree_kv_launch_count.argtypes = [C.c_void_p]
         L.opt_tree_strerror.restype = C.c_char_p
         L.opt_tree_strerror.argtypes = [C.c_int]
         _lib = L
@@ -297,3 +332,158 @@ def verify_static(cfg: Config, tree: Tree, target: torch.Tensor, root_token: tor
     _check(lib().opt_tree_verify_static(C.byref(cfg), C.byref(cs), _ptr(target), _ptr(root_token), B, _ptr(out[0]), _ptr(out[1]),
                                         _ptr(out[2]), _ptr(out[3]), _ptr(device_status), _stream()), "opt_tree_verify_static")
     return out
+
+
+# ---- the paged 8-bit cache of the target model's attention layers ----
+
+_ROW_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _plain(t, name: str, dtype, shape, device):
+    """A contiguous tensor of this type, shape and device (or None)."""
+    if t is not None and (t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr() if t is not None else None
+
+
+class KVCache:
+    """Cache tensors (torch owns the memory): k, v [layers][num_pages][kv_heads][page][head_dim] float8_e4m3fn, k_scale, v_scale
+    [layers][num_pages][kv_heads] float32, block_table [B][max_pages] int32 (see opt_tree_kv_cache)."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "block_table", "c")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor):
+        f8, dev = torch.float8_e4m3fn, k.device
+        if k.dim() != 5 or block_table.dim() != 2:
+            raise ValueError("k: [layers][num_pages][kv_heads][page][head_dim], block_table: [B][max_pages]")
+        self.c = KVCacheC(_plain(k, "k", f8, k.shape, dev), _plain(v, "v", f8, k.shape, dev),
+                          _plain(k_scale, "k_scale", torch.float32, k.shape[:3], dev), _plain(v_scale, "v_scale", torch.float32, k.shape[:3], dev),
+                          _plain(block_table, "block_table", torch.int32, block_table.shape, dev))
+        self.k, self.v, self.k_scale, self.v_scale, self.block_table = k, v, k_scale, v_scale, block_table
+
+
+class KVStep:
+    """A step's tokens (see opt_tree_kv_step): the root and `nodes` nodes of each sequence."""
+
+    __slots__ = ("kv_len", "nodes", "base_pos", "position_ids", "mask")
+
+    def __init__(self, kv_len: torch.Tensor, nodes: torch.Tensor | None = None, base_pos: torch.Tensor | None = None,
+                 position_ids: torch.Tensor | None = None, mask: torch.Tensor | None = None):
+        self.kv_len, self.nodes, self.base_pos, self.position_ids, self.mask = kv_len, nodes, base_pos, position_ids, mask
+
+    def c_struct(self, B: int, T: int, device) -> KVStepC:
+        i32, one = torch.int32, (B,)
+        return KVStepC(B, T, _plain(self.kv_len, "kv_len", i32, one, device), _plain(self.nodes, "nodes", i32, one, device),
+                       _plain(self.base_pos, "base_pos", i32, one, device), _plain(self.position_ids, "position_ids", i32, (B, T - 1), device),
+                       _plain(self.mask, "mask", torch.int64, (B, T - 1, (T + 62) // 64), device) if T > 1 else None)
+
+
+class TreeKV:
+    """A handle of the cache operators (opt_tree_kv_*): fixed sizes, workspace allocated once, on one device."""
+
+    def __init__(self, q_heads: int, kv_heads: int, head_dim: int, page: int, num_pages: int, max_pages: int, max_batch: int, max_step: int,
+                 layers: int = 1, dtype: torch.dtype = torch.bfloat16, device: str | torch.device | None = None):
+        self._kv = C.c_void_p()
+        if not torch.cuda.is_available():
+            raise RuntimeError("no CUDA device: the OPT-Tree library has no CPU fallback")
+        if dtype not in _ROW_TYPES:
+            raise ValueError(f"dtype: bfloat16 or float16, not {dtype}")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"device: a CUDA device, not {self.device}")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.dtype = dtype
+        self.cfg = KVConfig(q_heads, kv_heads, head_dim, page, num_pages, max_pages, max_batch, max_step, layers, _ROW_TYPES[dtype])
+        self._cache_shape = (layers, num_pages, kv_heads, page, head_dim)
+        self._scale = head_dim ** -0.5
+        with torch.cuda.device(self.device):
+            _check(lib().opt_tree_kv_create(C.byref(self._kv), C.byref(self.cfg)), "opt_tree_kv_create")
+
+    def close(self):
+        if self._kv:
+            lib().opt_tree_kv_destroy(self._kv)
+            self._kv = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def alloc_cache(self, block_table: torch.Tensor) -> KVCache:
+        L, N, H, P, D = self._cache_shape
+        k, v = (torch.zeros((L, N, H, P, D), dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn) for _ in range(2))
+        ks, vs = (torch.ones((L, N, H), dtype=torch.float32, device=self.device) for _ in range(2))
+        return KVCache(k, v, ks, vs, block_table)
+
+    def _rows(self, t: torch.Tensor, name: str, B: int, T: int, heads: int) -> KVRows:
+        if t.dtype != self.dtype or t.shape != (B, T, heads, self.cfg.head_dim) or t.device != self.device or t.stride(3) != 1:
+            raise ValueError(f"{name}: {self.dtype} [{B}][{T}][{heads}][{self.cfg.head_dim}] with contiguous rows on {self.device} is needed, "
+                             f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+        return KVRows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+    def _check_cache(self, cache: KVCache, B: int):
+        if cache.k.shape != self._cache_shape or cache.k.device != self.device or cache.block_table.shape[1] != self.cfg.max_pages or cache.block_table.shape[0] < B:
+            raise ValueError(f"cache: pages {self._cache_shape} and a block table [{B}][{self.cfg.max_pages}] on {self.device} are needed, "
+                             f"not {tuple(cache.k.shape)} and {tuple(cache.block_table.shape)} on {cache.k.device}")
+
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def append(self, cache: KVCache, layer: int, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, step: KVStep,
+               cos_sin: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
+               interleaved: bool = False, q_out: torch.Tensor | None = None) -> torch.Tensor | None:
+        """opt_tree_kv_append: norm and rotation of q and k, k and v into the cache; returns the rotated queries (q_out; None if q is None)."""
+        c, (B, T) = self.cfg, k.shape[:2]
+        self._check_cache(cache, B)
+        if q is not None and q_out is None:
+            q_out = torch.empty((B, T, c.q_heads, c.head_dim), dtype=self.dtype, device=self.device)
+        qr, qo = (C.byref(self._rows(t, n, B, T, c.q_heads)) if q is not None else None for t, n in ((q, "q"), (q_out, "q_out")))
+        turn = KVTurn(None, 0, 0, int(interleaved), _plain(q_norm, "q_norm", self.dtype, (c.head_dim,), self.device),
+                      _plain(k_norm, "k_norm", self.dtype, (c.head_dim,), self.device), eps)
+        if cos_sin is not None:
+            turn.cos_sin = _plain(cos_sin, "cos_sin", torch.float32, cos_sin.shape, self.device)
+            turn.positions, turn.rot_dim = cos_sin.shape
+        with torch.cuda.device(self.device):
+            _check(lib().opt_tree_kv_append(self._kv, C.byref(cache.c), layer, qr, C.byref(self._rows(k, "k", B, T, c.kv_heads)),
+                                            C.byref(self._rows(v, "v", B, T, c.kv_heads)), qo, C.byref(step.c_struct(B, T, self.device)),
+                                            C.byref(turn), self._stream()), "opt_tree_kv_append")
+        return q_out
+
+    def attend(self, cache: KVCache, layer: int, q: torch.Tensor, step: KVStep, scale: float | None = None, out: torch.Tensor | None = None,
+               lse: torch.Tensor | None = None) -> torch.Tensor:
+        """opt_tree_kv_attend: attention of the step's tokens over the cache; scale defaults to head_dim ** -0.5."""
+        c, (B, T) = self.cfg, q.shape[:2]
+        self._check_cache(cache, B)
+        if out is None:
+            out = torch.empty((B, T, c.q_heads, c.head_dim), dtype=self.dtype, device=self.device)
+        with torch.cuda.device(self.device):
+            _check(lib().opt_tree_kv_attend(self._kv, C.byref(cache.c), layer, C.byref(self._rows(q, "q", B, T, c.q_heads)),
+                                            C.byref(step.c_struct(B, T, self.device)), self._scale if scale is None else scale,
+                                            C.byref(self._rows(out, "out", B, T, c.q_heads)),
+                                            _plain(lse, "lse", torch.float32, (B, T, c.q_heads), self.device), self._stream()), "opt_tree_kv_attend")
+        return out
+
+    def compact(self, cache: KVCache, kv_len: torch.Tensor, kv_gather: torch.Tensor, kv_keep: torch.Tensor,
+                new_len: torch.Tensor | None = None) -> torch.Tensor:
+        """opt_tree_kv_compact: the accepted path's entries of all layers to the end of the prefix; returns the new lengths."""
+        B, G = kv_gather.shape
+        self._check_cache(cache, B)
+        if new_len is None:
+            new_len = torch.empty(B, dtype=torch.int32, device=self.device)
+        i32, dev = torch.int32, self.device
+        with torch.cuda.device(self.device):
+            _check(lib().opt_tree_kv_compact(self._kv, C.byref(cache.c), _plain(kv_len, "kv_len", i32, (B,), dev),
+                                             _plain(kv_gather, "kv_gather", i32, (B, G), dev), _plain(kv_keep, "kv_keep", i32, (B,), dev), G, B,
+                                             _plain(new_len, "new_len", i32, (B,), dev), self._stream()), "opt_tree_kv_compact")
+        return new_len
+
+    def device_status(self) -> int:
+        st = C.c_int32(0)
+        with torch.cuda.device(self.device):
+            _check(lib().opt_tree_kv_last_device_status(self._kv, C.byref(st)), "opt_tree_kv_last_device_status")
+        return st.value
+
+    def launch_count(self) -> int:
+        return int(lib().opt_tree_kv_launch_count(self._kv))

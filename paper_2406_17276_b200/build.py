@@ -8,24 +8,45 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libopt_tree.so")
-SOURCES = [os.path.join(CSRC, "opt_tree.cu")]
-NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-maxrregcount=80",
-              "-shared", "-Xcompiler", "-fPIC"]
+OBJECTS = os.path.join(_HERE, "_build")
+# Each source with its own flags (the tree kernels are all held to 80 registers, the cache kernels state theirs themselves) and the
+# headers it includes.
+TREE_HEADERS = ["common.cuh", "launch.cuh", "pipeline.cuh", "row_topk.cuh", "select.cuh"]
+KV_HEADERS = ["common.cuh", "launch.cuh", "kv_common.cuh", "kv_append.cuh", "kv_attend.cuh", "kv_compact.cuh"]
+SOURCES = [("opt_tree.cu", ["-maxrregcount=80"], TREE_HEADERS), ("kv.cu", [], KV_HEADERS)]
+NVCC = "/usr/local/cuda/bin/nvcc"
+ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
+NVCC_FLAGS = ARCH + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(_HERE, "..", "include", "opt_tree.h")]
-    return any(os.path.getmtime(d) > t for d in deps)
+def _older(target: str, deps) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(d) > os.path.getmtime(target) for d in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    if force or _stale():
-        nvcc = "/usr/local/cuda/bin/nvcc"
-        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + SOURCES
-        subprocess.check_call(cmd)
+    """Compiles what is older than its sources, the sources side by side, and links."""
+    api = os.path.join(_HERE, "..", "include", "opt_tree.h")
+    everything = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [api]
+    if not force and not _older(LIB, everything):
+        return LIB
+    os.makedirs(OBJECTS, exist_ok=True)
+    objects, jobs = [], []
+    for name, flags, headers in SOURCES:
+        src, obj = os.path.join(CSRC, name), os.path.join(OBJECTS, name + ".o")
+        objects.append(obj)
+        if force or _older(obj, [src, api, os.path.abspath(__file__)] + [os.path.join(CSRC, h) for h in headers]):
+            new = f"{obj}.{os.getpid()}.o"
+            cmd = [NVCC] + NVCC_FLAGS + flags + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", new, src]
+            jobs.append((subprocess.Popen(cmd), cmd, new, obj))
+    for proc, cmd, new, obj in jobs:
+        if proc.wait() != 0:
+            for other, *_ in jobs:
+                other.wait()
+            raise subprocess.CalledProcessError(proc.returncode, cmd)
+        os.replace(new, obj)
+    new = f"{LIB}.{os.getpid()}.so"
+    subprocess.check_call([NVCC] + ARCH + ["-shared", "-Xcompiler", "-fPIC", "-o", new] + objects)
+    os.replace(new, LIB)
     return LIB
 
 

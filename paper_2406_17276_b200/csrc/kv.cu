@@ -1,0 +1,214 @@
+// Host side of the cache operators (include/opt_tree.h: opt_tree_kv_*).
+#include <cstring>
+#include <new>
+
+#include "../../include/opt_tree.h"
+#include "kv_append.cuh"
+#include "kv_attend.cuh"
+#include "kv_compact.cuh"
+#include "launch.cuh"
+
+struct opt_tree_kv {
+    opt_tree_kv_config cfg;
+    ot::KvShape shape;
+    void* base;
+    int* status;
+    int device, sms;
+    int64_t launches;
+};
+
+namespace {
+
+bool valid_cfg(const opt_tree_kv_config* c) {
+    return c && c->q_heads >= 1 && c->kv_heads >= 1 && c->head_dim >= 1 && c->page >= 1 && c->num_pages >= 1 && c->max_pages >= 1 &&
+           c->max_batch >= 1 && c->max_step >= 1 && c->layers >= 1 && c->q_heads % c->kv_heads == 0 &&
+           (c->dtype == OPT_TREE_BF16 || c->dtype == OPT_TREE_FP16);
+}
+bool supported_cfg(const opt_tree_kv_config* c) {
+    if (c->head_dim != 64 && c->head_dim != 128) return false;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return false;
+    if (c->max_batch > 32767 || c->layers > 32767 || c->q_heads > 32767) return false;
+    if ((long long)c->max_pages * c->page > 1ll << 30) return false;                                   // slots of a sequence
+    if ((long long)c->max_batch * c->max_step * c->q_heads > 0x7FFFFFFFll) return false;               // rows of a step
+    const long long touched = (c->max_step + c->page - 2) / c->page + 1;
+    if ((long long)c->max_batch * touched * c->kv_heads * 2 > 0x3FFFFFFFll) return false;              // CTAs of an append
+    return true;
+}
+int check_launch() { return cudaGetLastError() == cudaSuccess ? OPT_TREE_OK : OPT_TREE_ERR_CUDA; }
+bool on_device(const opt_tree_kv* kv) {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == kv->device;
+}
+bool bad_cache(const opt_tree_kv_cache* c) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->block_table) return true;
+    return ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) != 0;
+}
+bool bad_step(const opt_tree_kv* kv, const opt_tree_kv_step* s) {
+    return !s || s->B < 1 || s->B > kv->cfg.max_batch || s->T < 1 || s->T > kv->cfg.max_step || !s->kv_len;
+}
+ot::KvStep step_of(const opt_tree_kv_step* s) { return ot::KvStep{s->B, s->T, s->kv_len, s->nodes, s->base_pos, s->position_ids, s->mask}; }
+ot::KvRows rows_of(const opt_tree_kv_rows* r) {
+    return ot::KvRows{static_cast<const uint16_t*>(r->data), (long long)r->batch, (long long)r->token, (long long)r->head};
+}
+bool bad_rows(const opt_tree_kv_rows* r) { return !r || !r->data || (reinterpret_cast<uintptr_t>(r->data) & 1u); }
+int wide(const opt_tree_kv_rows* r) {
+    return ((reinterpret_cast<uintptr_t>(r->data) & 15u) == 0 && r->batch % 8 == 0 && r->token % 8 == 0 && r->head % 8 == 0) ? 1 : 0;
+}
+
+using AppendKernel = void (*)(ot::KvAppend);
+// A CTA takes a page of one head and side: rows of head_dim / 8 lanes, so page * head_dim / 8 lanes in all, in at most four passes.
+template <int D, class T> AppendKernel append_variant(int page, int* threads) {
+    switch (page * D) {
+        case 1024: *threads = 128; return ot::kv_append_kernel<D, T, 128, 1>;
+        case 2048: *threads = 256; return ot::kv_append_kernel<D, T, 256, 1>;
+        case 4096: *threads = 256; return ot::kv_append_kernel<D, T, 256, 2>;
+        case 8192: *threads = 256; return ot::kv_append_kernel<D, T, 256, 4>;
+        default: *threads = 512; return ot::kv_append_kernel<D, T, 512, 4>;
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config* cfg) {
+    if (!valid_cfg(cfg) || !supported_cfg(cfg)) return 0;
+    return 256;
+}
+
+int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
+    if (!out) return OPT_TREE_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!valid_cfg(cfg)) return OPT_TREE_ERR_INVALID_ARG;
+    if (!supported_cfg(cfg)) return OPT_TREE_ERR_UNSUPPORTED;
+    opt_tree_kv* kv = new (std::nothrow) opt_tree_kv();
+    if (!kv) return OPT_TREE_ERR_CUDA;
+    kv->cfg = *cfg;
+    int shift = 0;
+    while ((1 << shift) < cfg->page) ++shift;
+    kv->shape = ot::KvShape{cfg->q_heads, cfg->kv_heads, cfg->page, cfg->num_pages, cfg->max_pages, shift};
+    const size_t bytes = opt_tree_kv_workspace_bytes(cfg);
+    if (cudaGetDevice(&kv->device) != cudaSuccess || cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, kv->device) != cudaSuccess ||
+        cudaMalloc(&kv->base, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        delete kv;
+        return OPT_TREE_ERR_CUDA;
+    }
+    if (cudaMemset(kv->base, 0, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(kv->base);
+        delete kv;
+        return OPT_TREE_ERR_CUDA;
+    }
+    kv->status = static_cast<int*>(kv->base);
+    *out = kv;
+    return OPT_TREE_OK;
+}
+
+int opt_tree_kv_destroy(opt_tree_kv* kv) {
+    if (!kv) return OPT_TREE_ERR_INVALID_ARG;
+    const cudaError_t e = cudaFree(kv->base);
+    delete kv;
+    return e == cudaSuccess ? OPT_TREE_OK : OPT_TREE_ERR_CUDA;
+}
+
+int opt_tree_kv_append(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t layer, const opt_tree_kv_rows* q, const opt_tree_kv_rows* k,
+                       const opt_tree_kv_rows* v, const opt_tree_kv_rows* q_out, const opt_tree_kv_step* step, const opt_tree_kv_turn* turn,
+                       void* stream) {
+    if (!kv || bad_cache(cache) || layer < 0 || layer >= kv->cfg.layers || bad_rows(k) || bad_rows(v) || bad_step(kv, step)) return OPT_TREE_ERR_INVALID_ARG;
+    if ((q != nullptr) != (q_out != nullptr) || (q && (bad_rows(q) || bad_rows(q_out)))) return OPT_TREE_ERR_INVALID_ARG;
+    opt_tree_kv_turn none;
+    memset(&none, 0, sizeof none);
+    if (!turn) turn = &none;
+    const int D = kv->cfg.head_dim;
+    if (turn->rot_dim < 0 || turn->rot_dim > D || turn->rot_dim % 16 || (turn->rot_dim && (!turn->cos_sin || turn->positions < 1)) ||
+        ((turn->q_norm || turn->k_norm) && !(turn->eps >= 0.f)) || ((reinterpret_cast<uintptr_t>(turn->cos_sin) & 3u) != 0) ||
+        (((reinterpret_cast<uintptr_t>(turn->q_norm) | reinterpret_cast<uintptr_t>(turn->k_norm)) & 1u) != 0))
+        return OPT_TREE_ERR_INVALID_ARG;
+    if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
+    ot::KvAppend a;
+    memset(&a, 0, sizeof a);
+    a.shape = kv->shape;
+    a.step = step_of(step);
+    a.k = rows_of(k); a.v = rows_of(v);
+    a.wide_k = wide(k); a.wide_v = wide(v);
+    if (q) { a.q = rows_of(q); a.q_out = rows_of(q_out); a.wide_q = wide(q); a.wide_out = wide(q_out); }
+    const long long layer_pages = (long long)layer * kv->cfg.num_pages * kv->cfg.kv_heads;
+    a.kc = cache->k + layer_pages * kv->cfg.page * D; a.vc = cache->v + layer_pages * kv->cfg.page * D;
+    a.ks = cache->k_scale + layer_pages; a.vs = cache->v_scale + layer_pages;
+    a.table = cache->block_table;
+    a.cos_sin = turn->cos_sin; a.positions = turn->positions; a.rot_dim = turn->rot_dim; a.interleaved = turn->interleaved ? 1 : 0;
+    a.q_norm = static_cast<const uint16_t*>(turn->q_norm); a.k_norm = static_cast<const uint16_t*>(turn->k_norm);
+    a.eps = turn->eps;
+    a.wide_w = ((reinterpret_cast<uintptr_t>(turn->q_norm) | reinterpret_cast<uintptr_t>(turn->k_norm)) & 15u) == 0;
+    a.page_slots = (step->T + kv->cfg.page - 2) / kv->cfg.page + 1;
+    a.page_blocks = step->B * a.page_slots * kv->cfg.kv_heads * 2;
+    a.by_heads = ot::FixedDiv::by((unsigned)kv->cfg.kv_heads); a.by_slots = ot::FixedDiv::by((unsigned)a.page_slots);
+    a.by_q_heads = ot::FixedDiv::by((unsigned)kv->cfg.q_heads); a.by_T = ot::FixedDiv::by((unsigned)step->T);
+    a.status = kv->status;
+    int threads = 0;
+    const bool bf16 = kv->cfg.dtype == OPT_TREE_BF16;
+    const AppendKernel kernel = D == 64 ? (bf16 ? append_variant<64, __nv_bfloat16>(kv->cfg.page, &threads) : append_variant<64, __half>(kv->cfg.page, &threads))
+                                        : (bf16 ? append_variant<128, __nv_bfloat16>(kv->cfg.page, &threads) : append_variant<128, __half>(kv->cfg.page, &threads));
+    const long long rows = q ? (long long)step->B * step->T * kv->cfg.q_heads : 0;
+    const long long per_block = (long long)(threads / 32) * (256 / D) * ot::kAppendQueryRows;
+    const long long blocks = a.page_blocks + (rows + per_block - 1) / per_block;
+    launch_after(kernel, dim3((unsigned)blocks), dim3(threads), 0, static_cast<cudaStream_t>(stream), a);
+    kv->launches++;
+    return check_launch();
+}
+
+int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t layer, const opt_tree_kv_rows* q, const opt_tree_kv_step* step,
+                       float scale, const opt_tree_kv_rows* out, float* lse, void* stream) {
+    if (!kv || bad_cache(cache) || layer < 0 || layer >= kv->cfg.layers || bad_rows(q) || bad_rows(out) || bad_step(kv, step) || !(scale > 0.f) ||
+        scale > 3.4e38f)
+        return OPT_TREE_ERR_INVALID_ARG;
+    if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
+    ot::KvAttend a;
+    memset(&a, 0, sizeof a);
+    const int D = kv->cfg.head_dim;
+    a.shape = kv->shape;
+    a.step = step_of(step);
+    a.q = rows_of(q); a.out = rows_of(out);
+    a.wide_q = wide(q); a.wide_out = wide(out);
+    const long long layer_pages = (long long)layer * kv->cfg.num_pages * kv->cfg.kv_heads;
+    a.kc = cache->k + layer_pages * kv->cfg.page * D; a.vc = cache->v + layer_pages * kv->cfg.page * D;
+    a.ks = cache->k_scale + layer_pages; a.vs = cache->v_scale + layer_pages;
+    a.table = cache->block_table;
+    a.lse = lse;
+    a.scale = scale;
+    a.status = kv->status;
+    const long long rows = (long long)step->B * step->T * kv->cfg.q_heads;
+    const bool bf16 = kv->cfg.dtype == OPT_TREE_BF16;
+    void (*kernel)(ot::KvAttend) = D == 64 ? (bf16 ? ot::kv_attend_plain_kernel<64, __nv_bfloat16> : ot::kv_attend_plain_kernel<64, __half>)
+                                           : (bf16 ? ot::kv_attend_plain_kernel<128, __nv_bfloat16> : ot::kv_attend_plain_kernel<128, __half>);
+    launch_after(kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, static_cast<cudaStream_t>(stream), a);
+    kv->launches++;
+    return check_launch();
+}
+
+int opt_tree_kv_compact(opt_tree_kv* kv, const opt_tree_kv_cache* cache, const int32_t* kv_len, const int32_t* kv_gather, const int32_t* kv_keep,
+                        int32_t G, int32_t B, int32_t* new_len, void* stream) {
+    if (!kv || bad_cache(cache) || !kv_len || !kv_gather || !kv_keep || G < 1 || B < 1 || B > kv->cfg.max_batch || new_len == kv_len)
+        return OPT_TREE_ERR_INVALID_ARG;
+    if (G > ot::kCompactMost) return OPT_TREE_ERR_UNSUPPORTED;
+    if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
+    ot::KvCompact a{kv->shape, cache->k, cache->v, cache->k_scale, cache->v_scale, cache->block_table, kv_len, kv_gather, kv_keep, G, new_len, kv->status};
+    launch_after(kv->cfg.head_dim == 64 ? ot::kv_compact_kernel<64> : ot::kv_compact_kernel<128>, dim3(B, kv->cfg.layers), dim3(ot::kCompactThreads), 0,
+                 static_cast<cudaStream_t>(stream), a);
+    kv->launches++;
+    return check_launch();
+}
+
+int opt_tree_kv_last_device_status(opt_tree_kv* kv, int32_t* status_host) {
+    if (!kv || !status_host) return OPT_TREE_ERR_INVALID_ARG;
+    if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
+    if (cudaDeviceSynchronize() != cudaSuccess) return OPT_TREE_ERR_CUDA;
+    if (cudaMemcpy(status_host, kv->status, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return OPT_TREE_ERR_CUDA;
+    if (cudaMemset(kv->status, 0, 4) != cudaSuccess) return OPT_TREE_ERR_CUDA;
+    return OPT_TREE_OK;
+}
+
+int64_t opt_tree_kv_launch_count(const opt_tree_kv* kv) { return kv ? kv->launches : 0; }
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "launch.cuh"
 #include "pipeline.cuh"
 #include "select.cuh"
 
@@ -1598,18 +1599,6 @@ ot::Params make_params(const opt_tree_ctx* ctx, const void* table, float delta) 
     p.delta = delta;
     p.aligned = ((reinterpret_cast<uintptr_t>(table) & 15u) == 0 && (c.V % 8) == 0) ? 1 : 0;
     return p;
-}
-// Launches a kernel that may be set up while the kernel before it in the stream drains (every kernel of
-// this library waits for its predecessor before it touches global memory, see grid_dependency_wait).
-template <class... KArgs, class... Args>
-void launch_after(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 // Threads of a verification CTA for (n + 1) * B rows (see kVerifyMany); `some`: rows per SM up to which CTAs of 256 are taken.
 int verify_threads(int n, int B, int sms, int some) {
