@@ -4,15 +4,17 @@
 
 #include "../../include/opt_tree.h"
 #include "kv_append.cuh"
-#include "kv_attend.cuh"
+#include "kv_attend_few.cuh"
 #include "kv_compact.cuh"
 #include "launch.cuh"
 
 struct opt_tree_kv {
     opt_tree_kv_config cfg;
     ot::KvShape shape;
-    void* base;
+    void* base;                          // status word, arrival counters, parts
     int* status;
+    int* arrived;
+    float* parts;
     int device, sms;
     int64_t launches;
 };
@@ -67,13 +69,37 @@ template <int D, class T> AppendKernel append_variant(int page, int* threads) {
     }
 }
 
+using AttendKernel = void (*)(ot::KvAttend);
+struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads; };
+template <int D, int NT, class T> AttendVariant few_variant() {
+    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads};
+}
+template <int D, class T> AttendVariant attend_variant(int rows) { return rows <= 8 ? few_variant<D, 1, T>() : few_variant<D, 2, T>(); }
+// The kernel for `rows` query rows per sequence and key head at most.
+AttendVariant attend_for(const opt_tree_kv_config& c, int rows) {
+    const bool bf16 = c.dtype == OPT_TREE_BF16;
+    if (c.head_dim == 64) return bf16 ? attend_variant<64, __nv_bfloat16>(rows) : attend_variant<64, __half>(rows);
+    return bf16 ? attend_variant<128, __nv_bfloat16>(rows) : attend_variant<128, __half>(rows);
+}
+const int kVariantRows[] = {1, 16};      // one row count for each variant
+constexpr size_t kMaxParts = 2;          // CTAs per SM at most
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+// Status word, arrival counters, and two parts for every CTA of the largest variant.
+size_t part_bytes(int head_dim) { return (size_t)ot::kv_part_floats<16, 128>() * 4 / (128 / head_dim) + 1024; }
+
 }  // namespace
 
 extern "C" {
 
 size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config* cfg) {
     if (!valid_cfg(cfg) || !supported_cfg(cfg)) return 0;
-    return 256;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        sms = 148;                                   // no device here: the size on a B200
+    }
+    return 256 + align256(sms * kMaxParts * sizeof(int)) + sms * kMaxParts * 2 * part_bytes(cfg->head_dim);
 }
 
 int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
@@ -100,7 +126,19 @@ int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
         delete kv;
         return OPT_TREE_ERR_CUDA;
     }
-    kv->status = static_cast<int*>(kv->base);
+    for (int rows : kVariantRows) {
+        const AttendVariant v = attend_for(*cfg, rows);
+        if (cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem) != cudaSuccess) {
+            cudaGetLastError();
+            cudaFree(kv->base);
+            delete kv;
+            return OPT_TREE_ERR_CUDA;
+        }
+    }
+    char* at = static_cast<char*>(kv->base);
+    kv->status = reinterpret_cast<int*>(at);
+    kv->arrived = reinterpret_cast<int*>(at + 256);
+    kv->parts = reinterpret_cast<float*>(at + 256 + align256(kv->sms * kMaxParts * sizeof(int)));
     *out = kv;
     return OPT_TREE_OK;
 }
@@ -176,13 +214,14 @@ int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
     a.ks = cache->k_scale + layer_pages; a.vs = cache->v_scale + layer_pages;
     a.table = cache->block_table;
     a.lse = lse;
-    a.scale = scale;
+    a.scale = scale * ot::kLog2e;
+    a.group = kv->cfg.q_heads / kv->cfg.kv_heads;
+    a.by_group = ot::FixedDiv::by((unsigned)a.group);
+    a.parts = kv->parts;
+    a.arrived = kv->arrived;
     a.status = kv->status;
-    const long long rows = (long long)step->B * step->T * kv->cfg.q_heads;
-    const bool bf16 = kv->cfg.dtype == OPT_TREE_BF16;
-    void (*kernel)(ot::KvAttend) = D == 64 ? (bf16 ? ot::kv_attend_plain_kernel<64, __nv_bfloat16> : ot::kv_attend_plain_kernel<64, __half>)
-                                           : (bf16 ? ot::kv_attend_plain_kernel<128, __nv_bfloat16> : ot::kv_attend_plain_kernel<128, __half>);
-    launch_after(kernel, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, static_cast<cudaStream_t>(stream), a);
+    const AttendVariant v = attend_for(kv->cfg, step->T * a.group);
+    launch_after(v.kernel, dim3(kv->sms * v.per_sm), dim3(v.threads), v.smem, static_cast<cudaStream_t>(stream), a);
     kv->launches++;
     return check_launch();
 }

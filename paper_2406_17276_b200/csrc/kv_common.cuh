@@ -109,6 +109,8 @@ __device__ __forceinline__ uint32_t recode4(uint32_t four, float ratio) {
 __device__ __forceinline__ uint4 recode16(uint4 v, float ratio) {
     return make_uint4(recode4(v.x, ratio), recode4(v.y, ratio), recode4(v.z, ratio), recode4(v.w, ratio));
 }
+// Orders this thread's accesses to shared memory before later asynchronous copies into it (and stores before tensor-core reads).
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // The exponent of the smallest power of two that brings amax to 448 (1.75 * 2^8) or below.
 __device__ __forceinline__ int scale_exponent(uint32_t amax_bits) {
