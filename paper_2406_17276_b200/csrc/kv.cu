@@ -5,6 +5,7 @@
 #include "../../include/opt_tree.h"
 #include "kv_append.cuh"
 #include "kv_attend_few.cuh"
+#include "kv_attend_tiles.cuh"
 #include "kv_compact.cuh"
 #include "launch.cuh"
 
@@ -70,23 +71,35 @@ template <int D, class T> AppendKernel append_variant(int page, int* threads) {
 }
 
 using AttendKernel = void (*)(ot::KvAttend);
-struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads; };
+using JoinKernel = void (*)(ot::KvAttend, int);
+struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads; JoinKernel join; };
 template <int D, int NT, class T> AttendVariant few_variant() {
-    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads};
+    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads, nullptr};
 }
-template <int D, class T> AttendVariant attend_variant(int rows) { return rows <= 8 ? few_variant<D, 1, T>() : few_variant<D, 2, T>(); }
+template <int D, class T> AttendVariant attend_variant(int rows) {
+    if (rows <= 8) return few_variant<D, 1, T>();
+    if (rows <= 16) return few_variant<D, 2, T>();
+    return AttendVariant{ot::kv_attend_tiles_kernel<D, T>, (size_t)ot::TileLayout<D>::kBytes, 1, ot::kTileThreads, ot::kv_join_kernel<D, T>};
+}
 // The kernel for `rows` query rows per sequence and key head at most.
 AttendVariant attend_for(const opt_tree_kv_config& c, int rows) {
     const bool bf16 = c.dtype == OPT_TREE_BF16;
     if (c.head_dim == 64) return bf16 ? attend_variant<64, __nv_bfloat16>(rows) : attend_variant<64, __half>(rows);
     return bf16 ? attend_variant<128, __nv_bfloat16>(rows) : attend_variant<128, __half>(rows);
 }
-const int kVariantRows[] = {1, 16};      // one row count for each variant
-constexpr size_t kMaxParts = 2;          // CTAs per SM at most
+const int kVariantRows[] = {1, 16, 17};  // one row count for each variant
+constexpr size_t kMaxParts = 2;          // CTAs per SM at most, and row tiles of a CTA
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-// Status word, arrival counters, and two parts for every CTA of the largest variant.
-size_t part_bytes(int head_dim) { return (size_t)ot::kv_part_floats<16, 128>() * 4 / (128 / head_dim) + 1024; }
+// Bytes of the two parts that each CTA may leave of a cut row tile, per SM: two CTAs with 16 rows each, or one with two tiles of 128.
+template <int D> size_t part_bytes(long long rows) {
+    const size_t few = (size_t)2 * 2 * ot::kv_part_floats<16, D>() * sizeof(float), tiles = (size_t)2 * 2 * ot::kv_part_floats<ot::kTileRows, D>() * sizeof(float);
+    return rows <= 16 ? few : tiles;
+}
+size_t parts_per_sm(const opt_tree_kv_config& c) {
+    const long long rows = (long long)c.max_step * (c.q_heads / c.kv_heads);
+    return c.head_dim == 64 ? part_bytes<64>(rows) : part_bytes<128>(rows);
+}
 
 }  // namespace
 
@@ -99,7 +112,7 @@ size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config* cfg) {
         cudaGetLastError();
         sms = 148;                                   // no device here: the size on a B200
     }
-    return 256 + align256(sms * kMaxParts * sizeof(int)) + sms * kMaxParts * 2 * part_bytes(cfg->head_dim);
+    return 256 + align256(sms * kMaxParts * sizeof(int)) + sms * parts_per_sm(*cfg);
 }
 
 int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
@@ -221,7 +234,12 @@ int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
     a.arrived = kv->arrived;
     a.status = kv->status;
     const AttendVariant v = attend_for(kv->cfg, step->T * a.group);
-    launch_after(v.kernel, dim3(kv->sms * v.per_sm), dim3(v.threads), v.smem, static_cast<cudaStream_t>(stream), a);
+    const int grid = kv->sms * v.per_sm;
+    launch_after(v.kernel, dim3(grid), dim3(v.threads), v.smem, static_cast<cudaStream_t>(stream), a);
+    if (v.join) {
+        launch_after(v.join, dim3(grid, ot::kJoinBlocks), dim3(256), 0, static_cast<cudaStream_t>(stream), a, grid);
+        kv->launches++;
+    }
     kv->launches++;
     return check_launch();
 }

@@ -50,12 +50,12 @@ struct KvRun {
     int first, last;                     // CTAs that hold the row tile's first and last tile: more than one if it is cut
 };
 
-// Walks the run of tiles of this CTA.  kRows rows and kKeys keys a tile.  Every warp keeps its own copy (no shared memory, no
+// Walks the run of tiles of one CTA of a grid.  kRows rows and kKeys keys a tile.  Every warp keeps its own copy (no shared memory, no
 // barrier); the lengths come from the cache after the first warp.
 template <int kRows, int kKeys>
 struct KvWalk {
     long long total, pos, end, base;     // tiles; base: first tile of sequence b
-    int grid, b;
+    int cta, grid, b;
 
     __device__ __forceinline__ static int row_tiles(const KvAttend& a, int tokens) { return (tokens * a.group + kRows - 1) / kRows; }
     // In a chain a row tile sees no further than its last token.
@@ -89,7 +89,7 @@ struct KvWalk {
         return v;
     }
     // false: nothing for this CTA.
-    __device__ bool begin(const KvAttend& a) {
+    __device__ bool begin(const KvAttend& a, int which, int ctas) {
         const int lane = threadIdx.x & 31;
         total = 0;
         long long incl = 0;
@@ -97,15 +97,21 @@ struct KvWalk {
             incl = warp_scan(sequence_tiles(a, b0 + lane));
             total += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
-        grid = (int)min((long long)gridDim.x, total);
-        if ((int)blockIdx.x >= grid) return false;
-        pos = total * blockIdx.x / grid;
-        end = total * (blockIdx.x + 1) / grid;
+        cta = which;
+        grid = (int)min((long long)ctas, total);
+        if (cta >= grid) return false;
+        pos = total * cta / grid;
+        end = total * (cta + 1) / grid;
+        find(a, incl);
+        return true;
+    }
+    // Sets b and base to the sequence that holds tile pos; incl: this lane's inclusive count where all sequences fit in a warp.
+    __device__ void find(const KvAttend& a, long long incl) {
+        const int lane = threadIdx.x & 31;
         base = 0;
         b = 0;
-        for (int b0 = 0; b0 < a.step.B; b0 += 32) {          // the sequence that holds tile pos
-            const long long mine = a.step.B <= 32 ? 0 : sequence_tiles(a, b0 + lane);
-            if (a.step.B > 32) incl = warp_scan(mine);
+        for (int b0 = 0; b0 < a.step.B; b0 += 32) {
+            if (a.step.B > 32) incl = warp_scan(sequence_tiles(a, b0 + lane));
             const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > pos);
             if (over) {
                 const int l = __ffs(over) - 1;
@@ -116,7 +122,12 @@ struct KvWalk {
             }
             base += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
-        return true;
+    }
+    // The row tile of this CTA's last key tile (k0, k1: that tile alone).
+    __device__ bool last(const KvAttend& a, KvRun& r) {
+        pos = end - 1;
+        find(a, a.step.B <= 32 ? warp_scan(sequence_tiles(a, threadIdx.x & 31)) : 0);
+        return next(a, r);
     }
     __device__ __forceinline__ int owner(long long tile) const { return (int)(((tile + 1) * grid - 1) / total); }
     // The next run; false at the end.
@@ -142,8 +153,8 @@ struct KvWalk {
         r.k0 = (int)off;
         r.k1 = (int)min((long long)n, off + (end - pos));
         const bool whole = r.k0 == 0 && r.k1 == n;
-        r.first = whole ? (int)blockIdx.x : owner(pos - off);
-        r.last = whole ? (int)blockIdx.x : owner(pos - off + n - 1);
+        r.first = whole ? cta : owner(pos - off);
+        r.last = whole ? cta : owner(pos - off + n - 1);
         pos += r.k1 - r.k0;
         return true;
     }
@@ -171,18 +182,31 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t four, uint32_t& seen) {
 // NaN values were met.
 template <int kRows, int D> __host__ __device__ constexpr int kv_part_floats() { return kRows * D + 2 * kRows + 4; }
 
-// Four outputs of one row to memory; `factor` normalises.
-template <class T>
-__device__ __forceinline__ void kv_store4(const KvAttend& a, const KvRun& r, int row, int d, int D, float4 x, bool nan) {
+// A row's outputs at elements [d, d + N) of query row `row` of the run (row tile included).
+template <int D, int N, class T>
+__device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int row, int d, float (&x)[N], bool nan) {
     const int token = (int)a.by_group.div((unsigned)row), hq = r.h * a.group + row - token * a.group;
     if (nan) {
-        x.x = kv_with_nan(a, r, token, d, D, x.x); x.y = kv_with_nan(a, r, token, d + 1, D, x.y);
-        x.z = kv_with_nan(a, r, token, d + 2, D, x.z); x.w = kv_with_nan(a, r, token, d + 3, D, x.w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = kv_with_nan(a, r, token, d + i, D, x[i]);
     }
     uint16_t* to = const_cast<uint16_t*>(a.out.data) + r.b * a.out.batch + token * a.out.token + hq * a.out.head + d;
-    const uint32_t lo = from_float2<T>(x.x, x.y), hi = from_float2<T>(x.z, x.w);
-    if (a.wide_out) *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
-    else { to[0] = (uint16_t)lo; to[1] = (uint16_t)(lo >> 16); to[2] = (uint16_t)hi; to[3] = (uint16_t)(hi >> 16); }
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = from_float2<T>(x[2 * i], x[2 * i + 1]);
+    if (!a.wide_out) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) { to[2 * i] = (uint16_t)w[i]; to[2 * i + 1] = (uint16_t)(w[i] >> 16); }
+    } else if (N % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i + 3 < N / 2; i += 4) *reinterpret_cast<uint4*>(to + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    } else if (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i + 1 < N / 2; i += 2) *reinterpret_cast<uint2*>(to + 2 * i) = make_uint2(w[i], w[i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) *reinterpret_cast<uint32_t*>(to + 2 * i) = w[i];
+    }
 }
 __device__ __forceinline__ void kv_store_lse(const KvAttend& a, const KvRun& r, int row, float m, float l) {
     if (!a.lse) return;
@@ -190,79 +214,71 @@ __device__ __forceinline__ void kv_store_lse(const KvAttend& a, const KvRun& r, 
     a.lse[((long long)r.b * a.step.T + token) * a.shape.q_heads + hq] = (m + log2f(l)) * kLn2;
 }
 
-// Called by all threads of a CTA after they have written their part of a cut row tile (slot: see below): the CTA that arrives last
-// joins the parts in the order of the keys.  Slots: 2c for the part with which CTA c begins, 2c + 1 for the one with which it ends
-// (a row tile that begins in c).  weights: kRows * grid floats at most are needed in parts; a chunk of pieces at a time is staged.
+// Slot of CTA c's part of a cut row tile: 2c for the tile with which it begins, 2c + 1 for the one with which it ends (which began
+// in c).
 __device__ __forceinline__ int kv_slot(const KvRun& r, int cta) { return cta == r.first ? 2 * cta + 1 : 2 * cta; }
 
-constexpr int kJoinChunk = 32;           // parts whose weights are staged together
-
-template <int kRows, int D, int kThreadsN, class T>
-__device__ void kv_join(const KvAttend& a, const KvRun& r, float* weights /* [kJoinChunk + 2][kRows] shared */, int* word /* shared */) {
-    __threadfence();                     // this thread's part of the part is visible before the arrival is
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const int pieces = r.last - r.first + 1;
-        const int before = atomicAdd(a.arrived + r.first, 1);
-        *word = before == pieces - 1;
-        if (before == pieces - 1) a.arrived[r.first] = 0;    // for the next call
+// Counts this CTA's part of a cut row tile as written; true to all kThreadsN threads of the one group that is the last.  They are
+// the threads of named barrier kBarrier and call this together after their stores.
+template <int kBarrier, int kThreadsN>
+__device__ __forceinline__ bool kv_last_part(int* arrived, int pieces, int* word /* shared */) {
+    __threadfence();                     // this thread's stores before the arrival
+    asm volatile("bar.sync %0, %1;" ::"n"(kBarrier), "n"(kThreadsN) : "memory");
+    if (threadIdx.x % kThreadsN == 0) {
+        const bool last = atomicAdd(arrived, 1) == pieces - 1;
+        if (last) *arrived = 0;          // for the next call
+        *word = last;
         __threadfence();
     }
-    __syncthreads();
-    if (!*word) return;
-    constexpr int kFloats = kv_part_floats<kRows, D>();
-    constexpr int kPer = kRows * D / 4, kMine = (kPer + kThreadsN - 1) / kThreadsN;
-    const int rows = min(kRows, r.tokens * a.group - r.rt * kRows);
-    float* top = weights + kJoinChunk * kRows;
-    float* sum = top + kRows;
-    for (int row = threadIdx.x; row < rows; row += kThreadsN) {
-        float m = -INFINITY;
-        for (int c = r.first; c <= r.last; ++c) m = fmaxf(m, __ldcg(a.parts + (long long)kv_slot(r, c) * kFloats + kRows * D + row));
-        m = m == -INFINITY ? 0.f : m;
-        top[row] = m;
-        sum[row] = 0.f;
-    }
-    __syncthreads();
-    float4 acc[kMine];
+    asm volatile("bar.sync %0, %1;" ::"n"(kBarrier), "n"(kThreadsN) : "memory");
+    return *word != 0;
+}
+// Joins a cut row tile's parts in the order of the keys: a warp a row, for the rows warp, warp + warps, ... of it.  kStep: parts from one
+// slot to the next.  row0: the tile's first row.
+template <int kRows, int D, class T>
+__device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
+    constexpr int kFloats = kv_part_floats<kRows, D>(), N = D / 32;
+    const int lane = threadIdx.x & 31, pieces = r.last - r.first + 1;
+    const long long step = (long long)kStep * kFloats;
+    auto part = [&](int i) { return parts + kv_slot(r, r.first + i) * step; };
+    int seen = 0;
+    for (int i = lane; i < pieces; i += 32) seen |= __ldcg(reinterpret_cast<const int*>(part(i)) + kRows * D + 2 * kRows);
+    const bool nan = __any_sync(0xFFFFFFFFu, seen != 0);
+    for (int row = warp; row < rows; row += warps) {
+        float top = -INFINITY, l = 0.f, x[N];
+        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, __ldcg(part(i) + kRows * D + row));
+        top = warp_max_f32(top);
+        if (top == -INFINITY) top = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    bool nan = false;
-    for (int c0 = r.first; c0 <= r.last; c0 += kJoinChunk) {
-        const int n = min(kJoinChunk, r.last + 1 - c0);
-        for (int i = threadIdx.x; i < n * kRows; i += kThreadsN) {
-            const int row = i % kRows;
-            if (row < rows) weights[i] = exp2f(__ldcg(a.parts + (long long)kv_slot(r, c0 + i / kRows) * kFloats + kRows * D + row) - top[row]);
-        }
-        __syncthreads();
-        for (int row = threadIdx.x; row < rows; row += kThreadsN) {
-            float s = sum[row];
-            for (int i = 0; i < n; ++i) s += weights[i * kRows + row] * __ldcg(a.parts + (long long)kv_slot(r, c0 + i) * kFloats + kRows * D + kRows + row);
-            sum[row] = s;
-        }
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float* part = a.parts + (long long)kv_slot(r, c0 + i) * kFloats;
-            nan = nan || __ldcg(reinterpret_cast<const int*>(part) + kRows * D + 2 * kRows) != 0;
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                const int at = (int)threadIdx.x + k * kThreadsN, row = at / (D / 4);
-                if (row >= rows) continue;
-                const float4 x = __ldcg(reinterpret_cast<const float4*>(part) + at);
-                const float w = weights[i * kRows + row];
-                acc[k].x += w * x.x; acc[k].y += w * x.y; acc[k].z += w * x.z; acc[k].w += w * x.w;
+        for (int e = 0; e < N; ++e) x[e] = 0.f;
+        for (int i0 = 0; i0 < pieces; i0 += 32) {
+            float w = 0.f;
+            if (i0 + lane < pieces) {
+                w = ex2_approx(__ldcg(part(i0 + lane) + kRows * D + row) - top);
+                l += w * __ldcg(part(i0 + lane) + kRows * D + kRows + row);
+            }
+            const int n = min(32, pieces - i0);
+#pragma unroll 8
+            for (int i = 0; i < n; ++i) {
+                const float f = __shfl_sync(0xFFFFFFFFu, w, i);
+                const float* at = part(i0 + i) + row * D + lane * N;
+                if (N == 4) {
+                    const float4 y = __ldcg(reinterpret_cast<const float4*>(at));
+                    x[0] += f * y.x; x[1] += f * y.y; x[2 % N] += f * y.z; x[3 % N] += f * y.w;
+                } else {
+                    const float2 y = __ldcg(reinterpret_cast<const float2*>(at));
+                    x[0] += f * y.x; x[1] += f * y.y;
+                }
             }
         }
-        __syncthreads();
-    }
 #pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-        const int at = (int)threadIdx.x + k * kThreadsN, row = at / (D / 4), d = at % (D / 4) * 4;
-        if (row >= rows) continue;
-        const float f = 1.f / sum[row];
-        kv_store4<T>(a, r, r.rt * kRows + row, d, D, make_float4(acc[k].x * f, acc[k].y * f, acc[k].z * f, acc[k].w * f), nan);
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+        const float f = 1.f / l;
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] *= f;
+        kv_store<D, N, T>(a, r, row0 + row, lane * N, x, nan);
+        if (lane == 0) kv_store_lse(a, r, row0 + row, top, l);
     }
-    for (int row = threadIdx.x; row < rows; row += kThreadsN) kv_store_lse(a, r, r.rt * kRows + row, top[row], sum[row]);
-    __syncthreads();
 }
 
 }  // namespace ot

@@ -23,7 +23,7 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Probabilities are rounded to half precision (2^-12 each) for the product with the values; they are held times 2^12 and times the
+// Probabilities are rounded to half precision (2^-11 of each at most) for the product with the values; they are held times 2^12 and times the
 // page's scale over the largest so far, so that pages with scales down to 2^-24 of the largest keep that accuracy.
 constexpr float kProbUnit = 4096.f;
 
@@ -35,7 +35,7 @@ template <int D, int NT> struct FewLayout {
     static constexpr int kRing = kFewWarps * kStages * kStage;
     static constexpr int kMerge = kFewWarps * (kRows * D + 2 * kRows) * 4;   // the warps' parts, over the ring
     static constexpr int kBig = kRing > kMerge ? kRing : kMerge;
-    static constexpr int kWeights = kBig, kBars = kWeights + (kJoinChunk + 2) * kRows * 4, kWord = kBars + kFewWarps * kStages * 8;
+    static constexpr int kBars = kBig, kWord = kBars + kFewWarps * kStages * 8;
     static constexpr int kBytes = kWord + 16;
 };
 
@@ -47,7 +47,6 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     unsigned char* ring = smem + warp * kStages * L::kStage;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + L::kBars) + warp * kStages;
-    float* weights = reinterpret_cast<float*>(smem + L::kWeights);
     int* word = reinterpret_cast<int*>(smem + L::kWord);
     if (lane == 0)
         for (int s = 0; s < kStages; ++s) mbar_init(bars + s, 1);
@@ -55,7 +54,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
     __syncwarp();
     grid_dependency_wait();
     KvWalk<kRows, kFewKeys> walk;
-    if (!walk.begin(a)) return;
+    if (!walk.begin(a, blockIdx.x, gridDim.x)) return;
     KvRun r;
     uint32_t count = 0;                                      // blocks this warp has consumed: its place in the ring
     bool dead = false;                                       // a wait ran out: nothing more is loaded
@@ -308,13 +307,15 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
                 if (d == 0) { part[kRows * D + row] = mm; part[kRows * D + kRows + row] = ll; }
             } else {
                 const float f = 1.f / ll;
-                kv_store4<T>(a, r, r.rt * kRows + row, d, D, make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), any_nan);
+                float x[4] = {sum.x * f, sum.y * f, sum.z * f, sum.w * f};
+                kv_store<D, 4, T>(a, r, r.rt * kRows + row, d, x, any_nan);
                 if (d == 0) kv_store_lse(a, r, r.rt * kRows + row, mm, ll);
             }
         }
         if (cut) {
             if (threadIdx.x == 0) reinterpret_cast<int*>(part)[kRows * D + 2 * kRows] = any_nan;
-            kv_join<kRows, D, kFewThreads, T>(a, r, weights, word);
+            if (kv_last_part<0, kFewThreads>(a.arrived + r.first, r.last - r.first + 1, word))
+                kv_join<kRows, D, T>(a, r, a.parts, 1, r.rt * kRows, rows, warp, kFewWarps);
         }
         proxy_fence();                                       // the ring is free again, for copies too
         __syncthreads();

@@ -1,0 +1,511 @@
+// Attention of many query rows (trees and chunks of prompts): row tiles of 2 x 128 on the tensor cores.
+//
+// Per tile of 128 keys: S = Q K^T (tcgen05, both operands from shared memory, fp32 in TMEM), softmax by the threads that own the rows, P in
+// half precision back to TMEM over S, O += P V with P from TMEM.  Two row tiles of 128 alternate, so that the tensor cores
+// work on one while the other's exponentials are taken.  Keys and values become half precision on their way into shared memory, where
+// e4m3 codes are exact: four warps load codes, convert, bring them to the largest page scale of the run (a power of two: exact
+// to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once per 256 rows.  (Eight-bit operands would need
+// queries and probabilities in two parts each: the same tensor time as half precision, and twice the conversions per row.)
+// One exponent per score: 16 a clock and SM, as long as both products of a tile take (2 * 128 * 128 * D at 4096 a clock for D =
+// 128); so neither side can be hidden behind the other much further.
+//
+// Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 conversion; warp 12 issues the products.  Barriers (all waits bounded):
+//   q      softmax -> products   queries of a run are in shared memory
+//   k, v   conversion <-> products, two stages each
+//   s[X]   products -> softmax X  scores of a key tile; all earlier products of X are complete, so O may be rescaled
+//   p[X]   softmax X -> products
+//   o[X]   products -> softmax X  the run's last product
+#pragma once
+
+#include <type_traits>
+
+#include "kv_attend.cuh"
+
+namespace ot {
+
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 13 * 32;
+
+// --- tcgen05 ---
+__device__ __forceinline__ void tmem_alloc(uint32_t* smem_word, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_word)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(unsigned long long* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, unsigned long long a, unsigned long long b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, unsigned long long b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t at, float (&x)[32]) {
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+                   "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+                   "=r"(r[30]), "=r"(r[31])
+                 : "r"(at));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&x)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(at), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]),
+                   "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]), "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]),
+                   "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]),
+                   "f"(x[30]), "f"(x[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]),
+                   "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory descriptor of a 128-byte-swizzled operand: rows of 128 bytes, eight rows an atom of 1024 bytes.  Along the summed index (K-major)
+// or along the other (MN-major); `block`: bytes from one 64-element block of the other index to the next (MN-major only).
+__device__ __forceinline__ unsigned long long tc_desc(uint32_t smem_address, uint32_t block) {
+    return (unsigned long long)(smem_address >> 4 & 0x3FFF) | (unsigned long long)(block >> 4) << 16 | (unsigned long long)(1024 >> 4) << 32 |
+           1ull << 46 | 2ull << 61;
+}
+// fp32 accumulators, half-precision operands, M = 128; mn: the second operand is MN-major.
+__host__ __device__ constexpr uint32_t tc_idesc(int n, bool mn) { return 1u << 4 | (mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }
+
+struct TileRun {                         // what the conversion warps find out about a run
+    float kmax, vmax;                    // largest page scales
+    int nan;                             // NaN codes among the step's values
+};
+constexpr int kTileRunSlots = 4;         // conversion is at most two key tiles, so two runs, ahead of the slower softmax's next run
+
+template <int D> struct TileLayout {
+    static constexpr int kOperand = 128 * D * 2;             // one half-precision operand of 128 rows
+    static constexpr int kQ = 0, kK = 2 * kOperand, kV = kK + 2 * kOperand, kBars = kV + 2 * kOperand;
+    enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 2,
+           kBarO = kBarP + 2, kBarEnd = kBarO + 2, kBarCount };
+    static constexpr int kRuns = kBars + kBarCount * 8, kMax = kRuns + kTileRunSlots * 16, kWords = kMax + 64, kUsed = kWords + 32;
+    static constexpr int kBytes = kUsed + 1024;              // the base is brought to a multiple of 1024
+    static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
+};
+
+// Bits of the slots that token i of a run's sequence sees among the step's tokens [j0, j0 + 32) (negative j: the prefix).
+__device__ __forceinline__ uint32_t kv_sees32(const KvStep& st, int b, int i, int tokens, int j0) {
+    const int end = tokens - j0;                             // bits at or beyond are behind the last slot
+    const uint32_t inside = end >= 32 ? 0xFFFFFFFFu : (end <= 0 ? 0u : (1u << end) - 1u);
+    if (!st.mask) {
+        const int n = i + 1 - j0;
+        return inside & (n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u));
+    }
+    uint32_t v = 0;
+    if (j0 <= 0) v = j0 <= -32 ? 0xFFFFFFFFu : (2u << -j0) - 1u;                   // the prefix and the root (j <= 0)
+    if (i > 0 && j0 > -32) {
+        const int W = (st.T - 1 + 63) >> 6, at = j0 - 1;
+        const uint64_t* m = st.mask + ((long long)b * (st.T - 1) + i - 1) * W;
+        if (at < 0) v |= -at < 32 ? (uint32_t)(m[0] << -at) : 0u;
+        else {
+            const int w = at >> 6, s = at & 63;
+            if (w < W) v |= (uint32_t)(m[w] >> s);
+            if (s > 32 && w + 1 < W) v |= (uint32_t)(m[w + 1] << (64 - s));
+        }
+    }
+    if (i >= j0 && i < j0 + 32) v |= 1u << (i - j0);
+    return v & inside;
+}
+
+// A row's sums are kept relative to a reference 2^10 below the largest score at the time; the largest may grow by another 2^5 before they
+// are brought to a new reference.  So probabilities of up to 2^15 use the range of half precision (rounded by 2^-11 of each down to 2^-24
+// of the largest; relative to the largest alone, small ones would lose bits that matter where the large ones' values cancel).
+constexpr float kLift = 10.f, kGrowth = 5.f;
+
+template <int D, class T>
+__global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const __grid_constant__ KvAttend a) {
+    using L = TileLayout<D>;
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char* smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + L::kBars);
+    TileRun* runs = reinterpret_cast<TileRun*>(smem + L::kRuns);
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + L::kWords);
+    if (warp == 12) {
+        if (lane == 0) {
+            mbar_init(bars + L::kBarQ, 8);
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(bars + L::kBarKFull + i, 4); mbar_init(bars + L::kBarKFree + i, 1);
+                mbar_init(bars + L::kBarVFull + i, 4); mbar_init(bars + L::kBarVFree + i, 1);
+                mbar_init(bars + L::kBarS + i, 1); mbar_init(bars + L::kBarP + i, 4); mbar_init(bars + L::kBarO + i, 1);
+            }
+            mbar_init(bars + L::kBarEnd, 1);
+            mbar_fence_init();
+        }
+        __syncwarp();
+        tmem_alloc(words, L::kColumns);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = words[0];
+    grid_dependency_wait();
+    // A wait that runs out is recorded; from then on this warp waits for nothing more but goes through its work, so that barriers and
+    // counters stay in step and the kernel ends.
+    bool dead = false;
+    auto wait = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_warp(bars + bar, parity, a.status); };
+    KvWalk<2 * kTileRows, kTileKeys> walk;
+    KvRun r;
+    const bool any = walk.begin(a, blockIdx.x, gridDim.x);
+    if (!any) {
+    } else if (warp < 8) {
+        // ---- softmax: a thread a row ----
+        const int X = warp >> 2, in_tile = threadIdx.x & 127;
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) * 32u << 16);
+        const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
+        uint32_t tiles = 0, outs = 0, runs_seen = 0;
+        int slot = 0;
+        while (walk.next(a, r)) {
+            const int row0 = r.rt * 2 * kTileRows + X * kTileRows, rows = min(kTileRows, r.tokens * a.group - row0);   // rows <= 0: none for X
+            const int row = row0 + in_tile;
+            const bool mine = in_tile < rows, busy = (warp & 3) * 32 < rows;       // this thread, this warp
+            const int token = (int)a.by_group.div((unsigned)min(row, r.tokens * a.group - 1));
+            // queries to shared memory; bf16 rows are brought to half precision by a power of two of their own (exact but for
+            // elements below 2^-22 of the row's largest)
+            float qf = a.scale;
+            if (rows > 0) {
+                uint4 q[D / 8];
+                if (mine) {
+                    const int hq = r.h * a.group + row - token * a.group;
+                    const uint16_t* from = a.q.data + r.b * a.q.batch + token * a.q.token + hq * a.q.head;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) q[i] = load8(from + i * 8, a.wide_q);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) q[i] = make_uint4(0, 0, 0, 0);
+                }
+                float f = 1.f;
+                if (!std::is_same<T, __half>::value) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, w[e] >> 16 & 0x7FFFu));
+                    }
+                    const int e = min(max((int)(top >> 7) - 127, -112), 120);
+                    f = power_of_two(8 - e);
+                    qf *= power_of_two(e - 8);
+                }
+                unsigned char* at = smem + L::kQ + X * L::kOperand + in_tile * 128;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    uint32_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 y = to_float2<T>(w[e]);
+                        h[e] = std::is_same<T, __half>::value ? w[e] : from_float2<__half>(y.x * f, y.y * f);
+                    }
+                    *reinterpret_cast<uint4*>(at + (i >> 3) * (128 * 128) + (((i & 7) ^ (in_tile & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            }
+            proxy_fence();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + L::kBarQ);
+            const TileRun* run = runs + slot;
+            slot = (slot + 1) & (kTileRunSlots - 1);
+            if (rows <= 0) {                                 // in step with the others: one arrival a run
+                wait(L::kBarQ, runs_seen++ & 1);
+                continue;
+            }
+            ++runs_seen;
+            float m = -INFINITY, l = 0.f;
+            for (int kt = r.k0; kt < r.k1; ++kt, ++tiles) {
+                wait(L::kBarS + X, tiles & 1);
+                tc_fence_after();
+                if (busy) {
+                    const float f = fmaxf(qf * run->kmax, 1.2e-38f);
+                    const int j0 = kt * kTileKeys - r.len;   // the tile's first slot, as a token of the step
+                    const bool edge = j0 + kTileKeys > 0;
+                    float x[32], top = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_load32(ts + c * 32, x);
+                        if (edge) {
+                            const uint32_t see = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = see >> i & 1 ? x[i] : -INFINITY;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i]);
+                    }
+                    top *= f;
+                    const float was = m;
+                    const bool grows = top > m + (kLift + kGrowth);          // (the first score that is seen, too)
+                    if (grows) m = top - kLift;
+                    if (__any_sync(0xFFFFFFFFu, grows) && kt > r.k0) {
+                        const float fade = grows ? ex2_approx(was - m) : 1.f;
+                        l *= fade;
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            tmem_load32(to + c * 32, x);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] *= fade;
+                            tmem_store32(to + c * 32, x);
+                        }
+                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+                    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_load32(ts + c * 32, x);
+                        if (edge) {
+                            const uint32_t see = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = see >> i & 1 ? x[i] : -INFINITY;
+                        }
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float e0 = ex2_approx(fmaf(x[2 * i], f, -base)), e1 = ex2_approx(fmaf(x[2 * i + 1], f, -base));
+                            sum0 += e0; sum1 += e1;
+                            p[i] = from_float2<__half>(e0, e1);
+                        }
+                        tmem_store16(ts + c * 16, p);
+                    }
+                    l += sum0 + sum1;
+                    tmem_wait_stores();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + L::kBarP + X);
+            }
+            wait(L::kBarO + X, outs & 1);
+            ++outs;
+            tc_fence_after();
+            const bool cut = r.first != r.last;
+            constexpr int kFloats = kv_part_floats<kTileRows, D>();
+            float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + X) * kFloats;
+            const bool nan = run->nan != 0;
+            const float unit = cut ? run->vmax : run->vmax / l;
+            if (busy) {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    float x[32];
+                    tmem_load32(to + c * 32, x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[i] *= unit;
+                    if (!mine) continue;
+                    if (cut) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            *reinterpret_cast<float4*>(part + in_tile * D + c * 32 + i * 4) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    } else {
+                        kv_store<D, 32, T>(a, r, row, c * 32, x, nan);
+                    }
+                }
+                if (mine && cut) { part[kTileRows * D + in_tile] = m; part[kTileRows * D + kTileRows + in_tile] = l; }
+                if (mine && !cut) kv_store_lse(a, r, row, m, l);
+            }
+            tc_fence_before();
+            if (cut && in_tile == 0) reinterpret_cast<int*>(part)[kTileRows * D + 2 * kTileRows] = nan;
+        }
+    } else if (warp < 12) {
+        // ---- conversion: codes to half precision, in the layout of the products ----
+        constexpr int kLanes = D / 16, kAtOnce = 128 / kLanes, kIter = 128 / kAtOnce;   // 16 codes a lane; keys at once
+        const int tid = threadIdx.x - 256, sub = tid & (kLanes - 1), key = tid / kLanes;
+        float* most = reinterpret_cast<float*>(smem + L::kMax);
+        uint32_t done = 0;                                   // key tiles converted so far
+        int slot = 0;
+        const int shift = a.shape.page_shift, inside = a.shape.page - 1;
+        while (walk.next(a, r)) {
+            const int end = r.len + r.tokens;                // slots at or beyond it are not read
+            int id[kIter];
+            auto look = [&](int kt) {
+#pragma unroll
+                for (int i = 0; i < kIter; ++i) {
+                    const int s = kt * kTileKeys + i * kAtOnce + key;
+                    id[i] = s < end ? max(0, kv_page(a.shape, a.table, r.b, s >> shift, a.status)) : -1;
+                }
+            };
+            auto load = [&](const uint8_t* side, const float* scales, int kt, uint4 (&x)[kIter], float (&sc)[kIter]) {
+#pragma unroll
+                for (int i = 0; i < kIter; ++i) {
+                    x[i] = make_uint4(0, 0, 0, 0);
+                    sc[i] = 0.f;
+                    if (id[i] >= 0) {
+                        const int s = kt * kTileKeys + i * kAtOnce + key;
+                        const long long head = (long long)id[i] * a.shape.kv_heads + r.h;
+                        x[i] = ld_nc_v4(reinterpret_cast<const uint4*>(side + (head * a.shape.page + (s & inside)) * D + sub * 16));
+                        sc[i] = __ldg(scales + head);
+                    }
+                }
+            };
+            uint4 kx[kIter], vx[kIter];
+            float ksc[kIter], vsc[kIter];
+            look(r.k0);
+            load(a.kc, a.ks, r.k0, kx, ksc);
+            // the largest scales of the run's pages
+            float kmax = 0.f, vmax = 0.f;
+            const int p1 = (min(end, r.k1 * kTileKeys) - 1) >> shift;
+            for (int p = (r.k0 * kTileKeys >> shift) + tid; p <= p1; p += 128) {
+                const long long head = (long long)max(0, kv_page(a.shape, a.table, r.b, p, a.status)) * a.shape.kv_heads + r.h;
+                kmax = fmaxf(kmax, __ldg(a.ks + head)); vmax = fmaxf(vmax, __ldg(a.vs + head));
+            }
+            kmax = warp_max_f32(kmax); vmax = warp_max_f32(vmax);
+            if (lane == 0) { most[(warp - 8) * 2] = kmax; most[(warp - 8) * 2 + 1] = vmax; }
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+#pragma unroll
+            for (int w = 0; w < 4; ++w) { kmax = fmaxf(kmax, most[w * 2]); vmax = fmaxf(vmax, most[w * 2 + 1]); }
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+            TileRun* run = runs + slot;
+            slot = (slot + 1) & (kTileRunSlots - 1);
+            const float kinv = 1.f / kmax, vinv = 1.f / vmax;
+            auto write = [&](unsigned char* to, const uint4 (&x)[kIter], const float (&sc)[kIter], float inv) {
+#pragma unroll
+                for (int i = 0; i < kIter; ++i) {
+                    const int row = i * kAtOnce + key;
+                    const __half2 f = __float2half2_rn(sc[i] * inv);
+                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                    uint32_t h[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t two = from_e4m3x2((uint16_t)(w[e >> 1] >> (e & 1) * 16));
+                        const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&two), f);
+                        h[e] = *reinterpret_cast<const uint32_t*>(&y);
+                    }
+                    // two chunks of eight elements; lanes of the second 64 elements begin with the other one, whose banks are free
+                    const int block = sub >> 2, chunk = (sub & 3) * 2;
+                    unsigned char* base = to + block * (128 * 128) + row * 128;
+                    const uint4 c0 = make_uint4(h[0], h[1], h[2], h[3]), c1 = make_uint4(h[4], h[5], h[6], h[7]);
+                    *reinterpret_cast<uint4*>(base + (((chunk + block) ^ (row & 7)) << 4)) = block ? c1 : c0;
+                    *reinterpret_cast<uint4*>(base + (((chunk + 1 - block) ^ (row & 7)) << 4)) = block ? c0 : c1;
+                }
+            };
+            for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
+                const uint32_t stage = done & 1, phase = done >> 1 & 1;
+                load(a.vc, a.vs, kt, vx, vsc);
+                wait(L::kBarKFree + stage, phase ^ 1);
+                if (kt == r.k0) {                            // the slot's last run is over (see kTileRunSlots)
+                    if (tid == 0) { run->kmax = kmax; run->vmax = vmax; run->nan = 0; }
+                    asm volatile("bar.sync 3, 128;" ::: "memory");
+                }
+                write(smem + L::kK + stage * L::kOperand, kx, ksc, kinv);
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + L::kBarKFull + stage);
+                if (kt + 1 < r.k1) { look(kt + 1); load(a.kc, a.ks, kt + 1, kx, ksc); }
+                if ((kt + 1) * kTileKeys > r.len) {          // NaN codes of the step's own values
+                    uint32_t seen = 0;
+#pragma unroll
+                    for (int i = 0; i < kIter; ++i)
+                        if (kt * kTileKeys + i * kAtOnce + key >= r.len) {
+                            vx[i].x = drop_nan(vx[i].x, seen); vx[i].y = drop_nan(vx[i].y, seen);
+                            vx[i].z = drop_nan(vx[i].z, seen); vx[i].w = drop_nan(vx[i].w, seen);
+                        }
+                    if (seen) atomicOr(&run->nan, 1);
+                }
+                wait(L::kBarVFree + stage, phase ^ 1);
+                write(smem + L::kV + stage * L::kOperand, vx, vsc, vinv);
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + L::kBarVFull + stage);
+            }
+        }
+    } else {
+        // ---- products: one lane issues ----
+        constexpr uint32_t kScores = tc_idesc(kTileKeys, false), kOutputs = tc_idesc(D, true);
+        const uint32_t sq = smem_u32(smem + L::kQ), sk = smem_u32(smem + L::kK), sv = smem_u32(smem + L::kV);
+        uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
+        auto scores = [&](int X, uint32_t stage) {
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t at = (k >> 2) * (128 * 128) + (k & 3) * 32;
+                    tc_mma_ss(tmem + L::kColS + X * 128, tc_desc(sq + X * L::kOperand + at, 16), tc_desc(sk + stage * L::kOperand + at, 16), kScores, k > 0);
+                }
+                tc_commit(bars + L::kBarS + X);
+            }
+            __syncwarp();
+        };
+        while (walk.next(a, r)) {
+            const int left = r.tokens * a.group - r.rt * 2 * kTileRows;
+            const int X1 = left > kTileRows ? 2 : 1;
+            wait(L::kBarQ, nrun & 1);
+            ++nrun;
+            wait(L::kBarKFull + (done & 1), done >> 1 & 1);
+            tc_fence_after();
+            for (int X = 0; X < X1; ++X) scores(X, done & 1);
+            if (lane == 0) tc_commit(bars + L::kBarKFree + (done & 1));
+            for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
+                const uint32_t stage = done & 1, next = (done + 1) & 1;
+                const bool more = kt + 1 < r.k1;
+                wait(L::kBarVFull + stage, done >> 1 & 1);
+                for (int X = 0; X < X1; ++X) {
+                    wait(L::kBarP + X, tiles[X] & 1);
+                    ++tiles[X];
+                    tc_fence_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int k = 0; k < kTileKeys / 16; ++k)
+                            tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + k * 8, tc_desc(sv + stage * L::kOperand + k * 2048, 128 * 128), kOutputs,
+                                      kt > r.k0 || k > 0);
+                        if (!more) tc_commit(bars + L::kBarO + X);
+                    }
+                    __syncwarp();
+                    if (more) {
+                        if (X == 0) {
+                            wait(L::kBarKFull + next, (done + 1) >> 1 & 1);
+                            tc_fence_after();
+                        }
+                        scores(X, next);
+                    }
+                }
+                if (lane == 0) {
+                    tc_commit(bars + L::kBarVFree + stage);
+                    if (more) tc_commit(bars + L::kBarKFree + next);
+                }
+                __syncwarp();
+            }
+        }
+        // everything issued is complete before TMEM is given back, also after a wait that ran out
+        if (lane == 0) tc_commit(bars + L::kBarEnd);
+        __syncwarp();
+        mbar_wait_warp(bars + L::kBarEnd, 0, a.status);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) tmem_free(tmem, L::kColumns);
+}
+
+// Joins the parts of the row tiles that the kernel above has cut: block (c, j) takes rows j, j + kJoinBlocks, ... (of each eight) of the tile that
+// began in CTA c.  A kernel of its own, because there is much to read (64 KB a part at D = 128) and the CTA that finished last would be
+// alone with it.
+constexpr int kJoinBlocks = 16;
+
+template <int D, class T>
+__global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttend a, int grid) {
+    grid_dependency_wait();
+    KvWalk<2 * kTileRows, kTileKeys> walk;
+    KvRun r;
+    if (!walk.begin(a, blockIdx.x, grid) || !walk.last(a, r)) return;
+    if (r.first == r.last || r.first != (int)blockIdx.x) return;
+    constexpr int kFloats = kv_part_floats<kTileRows, D>();
+    const int warp = threadIdx.x >> 5;
+    for (int X = 0; X < 2; ++X) {
+        const int row0 = r.rt * 2 * kTileRows + X * kTileRows, rows = min(kTileRows, r.tokens * a.group - row0);
+        kv_join<kTileRows, D, T>(a, r, a.parts + (long long)X * kFloats, 2, row0, rows, blockIdx.y * 8 + warp, kJoinBlocks * 8);
+    }
+}
+
+}  // namespace ot

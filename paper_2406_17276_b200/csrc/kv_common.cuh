@@ -86,6 +86,12 @@ template <class T> __device__ __forceinline__ void unpack8(uint4 v, float (&x)[8
     }
 }
 
+__device__ __forceinline__ uint4 ld_nc_v4(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 // --- e4m3 ---
 // Two values to two codes (round to nearest even, saturating, NaN stays NaN), `lo` in the low byte.
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
