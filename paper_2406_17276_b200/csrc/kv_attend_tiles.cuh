@@ -9,12 +9,14 @@
 // One exponent per score: 16 a clock and SM, as long as both products of a tile take (2 * 128 * 128 * D at 4096 a clock for D =
 // 128); so neither side can be hidden behind the other much further.
 //
-// Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 conversion; warp 12 issues the products.  Barriers (all waits bounded):
-//   q      softmax -> products   queries of a run are in shared memory
-//   k, v   conversion <-> products, two stages each
-//   s[X]   products -> softmax X  scores of a key tile; all earlier products of X are complete, so O may be rescaled
-//   p[X]   softmax X -> products
-//   o[X]   products -> softmax X  the run's last product
+// Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 conversion; warp 12 issues the products; warp 13 looks pages up and
+// copies their codes into shared memory a key tile ahead.  Barriers (all waits bounded):
+//   q          softmax -> products      queries of a run are in shared memory
+//   rk, rv     copies <-> conversion    codes of a key tile
+//   k, v       conversion <-> products  operands, two stages each
+//   s[X]       products -> softmax X    scores of a key tile; all earlier products of X are complete, so O may be rescaled
+//   p[X]       softmax X -> products
+//   o[X]       products -> softmax X    the run's last product
 #pragma once
 
 #include <type_traits>
@@ -23,7 +25,7 @@
 
 namespace ot {
 
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 13 * 32;
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 14 * 32;
 
 // --- tcgen05 ---
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_word, uint32_t columns) {
@@ -85,21 +87,33 @@ __device__ __forceinline__ unsigned long long tc_desc(uint32_t smem_address, uin
 // fp32 accumulators, half-precision operands, M = 128; mn: the second operand is MN-major.
 __host__ __device__ constexpr uint32_t tc_idesc(int n, bool mn) { return 1u << 4 | (mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }
 
-struct TileRun {                         // what the conversion warps find out about a run
-    float kmax, vmax;                    // largest page scales
-    int nan;                             // NaN codes among the step's values
+// What the copying warp finds out about a key tile.  Keys of a tile are brought to the tile's largest scale, values to one reference that
+// outputs are kept in: the first tile's largest scale, or a later one's that is over 64 times the reference so far (64 * 448 is within
+// half precision).
+struct TileInfo {
+    uint32_t kratio[8], vratio[8];       // of each 16 keys, twice in half precision
+    float kmax;
+    float fade, ref;                     // factor for the outputs so far, reference of the values
+    float pad;
 };
-constexpr int kTileRunSlots = 4;         // conversion is at most two key tiles, so two runs, ahead of the slower softmax's next run
+// Slots of TileInfo, by tile, and of the NaN word, by run.  The copying warp writes those of tile t (of run r) once the codes of tile t - 2 at
+// least have been taken; then values of t - 3 have been written, so the products of t - 5 are complete, so both softmax groups are done with
+// tile t - 5, and done with the run before that tile's.
+constexpr int kTileSlots = 8;
 
 template <int D> struct TileLayout {
     static constexpr int kOperand = 128 * D * 2;             // one half-precision operand of 128 rows
-    static constexpr int kQ = 0, kK = 2 * kOperand, kV = kK + 2 * kOperand, kBars = kV + 2 * kOperand;
+    static constexpr int kCodes = 128 * D, kRaw = D == 128 ? 1 : 2;          // codes of one side of a key tile; stages of them
+    static constexpr int kQ = 0, kK = 2 * kOperand, kV = kK + 2 * kOperand, kRawK = kV + 2 * kOperand, kRawV = kRawK + kRaw * kCodes;
+    static constexpr int kBars = kRawV + kRaw * kCodes;
     enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 2,
-           kBarO = kBarP + 2, kBarEnd = kBarO + 2, kBarCount };
-    static constexpr int kRuns = kBars + kBarCount * 8, kMax = kRuns + kTileRunSlots * 16, kWords = kMax + 64, kUsed = kWords + 32;
-    static constexpr int kBytes = kUsed + 1024;              // the base is brought to a multiple of 1024
+           kBarO = kBarP + 2, kBarRKFull = kBarO + 2, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
+           kBarEnd = kBarRVFree + kRaw, kBarCount };
+    static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4;
+    static constexpr int kBytes = kWord + 16 + 1024;         // the base is brought to a multiple of 1024
     static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
 };
+static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
 
 // Bits of the slots that token i of a run's sequence sees among the step's tokens [j0, j0 + 32) (negative j: the prefix).
 __device__ __forceinline__ uint32_t kv_sees32(const KvStep& st, int b, int i, int tokens, int j0) {
@@ -137,8 +151,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     unsigned char* smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + L::kBars);
-    TileRun* runs = reinterpret_cast<TileRun*>(smem + L::kRuns);
-    uint32_t* words = reinterpret_cast<uint32_t*>(smem + L::kWords);
+    TileInfo* infos = reinterpret_cast<TileInfo*>(smem + L::kInfo);
+    int* nans = reinterpret_cast<int*>(smem + L::kNan);
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + L::kWord);
     if (warp == 12) {
         if (lane == 0) {
             mbar_init(bars + L::kBarQ, 8);
@@ -146,6 +161,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 mbar_init(bars + L::kBarKFull + i, 4); mbar_init(bars + L::kBarKFree + i, 1);
                 mbar_init(bars + L::kBarVFull + i, 4); mbar_init(bars + L::kBarVFree + i, 1);
                 mbar_init(bars + L::kBarS + i, 1); mbar_init(bars + L::kBarP + i, 4); mbar_init(bars + L::kBarO + i, 1);
+            }
+            for (int i = 0; i < L::kRaw; ++i) {
+                mbar_init(bars + L::kBarRKFull + i, 1); mbar_init(bars + L::kBarRKFree + i, 4);
+                mbar_init(bars + L::kBarRVFull + i, 1); mbar_init(bars + L::kBarRVFree + i, 4);
             }
             mbar_init(bars + L::kBarEnd, 1);
             mbar_fence_init();
@@ -171,8 +190,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         const int X = warp >> 2, in_tile = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) * 32u << 16);
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
-        uint32_t tiles = 0, outs = 0, runs_seen = 0;
-        int slot = 0;
+        uint32_t tiles = 0, outs = 0, runs_seen = 0, at = 0;     // at: key tiles of all runs, also those without rows for X
         while (walk.next(a, r)) {
             const int row0 = r.rt * 2 * kTileRows + X * kTileRows, rows = min(kTileRows, r.tokens * a.group - row0);   // rows <= 0: none for X
             const int row = row0 + in_tile;
@@ -221,19 +239,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             proxy_fence();
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + L::kBarQ);
-            const TileRun* run = runs + slot;
-            slot = (slot + 1) & (kTileRunSlots - 1);
+            const int run = (int)runs_seen++;
             if (rows <= 0) {                                 // in step with the others: one arrival a run
-                wait(L::kBarQ, runs_seen++ & 1);
+                wait(L::kBarQ, run & 1);
+                at += r.k1 - r.k0;
                 continue;
             }
-            ++runs_seen;
-            float m = -INFINITY, l = 0.f;
-            for (int kt = r.k0; kt < r.k1; ++kt, ++tiles) {
+            float m = -INFINITY, l = 0.f, ref = 1.f;
+            for (int kt = r.k0; kt < r.k1; ++kt, ++tiles, ++at) {
                 wait(L::kBarS + X, tiles & 1);
                 tc_fence_after();
                 if (busy) {
-                    const float f = fmaxf(qf * run->kmax, 1.2e-38f);
+                    const TileInfo& info = infos[at & (kTileSlots - 1)];
+                    const float f = fmaxf(qf * info.kmax, 1.2e-38f), unit = info.fade;
+                    ref = info.ref;
                     const int j0 = kt * kTileKeys - r.len;   // the tile's first slot, as a token of the step
                     const bool edge = j0 + kTileKeys > 0;
                     float x[32], top = -INFINITY;
@@ -252,9 +271,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     const float was = m;
                     const bool grows = top > m + (kLift + kGrowth);          // (the first score that is seen, too)
                     if (grows) m = top - kLift;
-                    if (__any_sync(0xFFFFFFFFu, grows) && kt > r.k0) {
-                        const float fade = grows ? ex2_approx(was - m) : 1.f;
+                    if (kt > r.k0 && (unit != 1.f || __any_sync(0xFFFFFFFFu, grows))) {
+                        float fade = grows ? ex2_approx(was - m) : 1.f;
                         l *= fade;
+                        fade *= unit;
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c) {
                             tmem_load32(to + c * 32, x);
@@ -295,8 +315,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             const bool cut = r.first != r.last;
             constexpr int kFloats = kv_part_floats<kTileRows, D>();
             float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + X) * kFloats;
-            const bool nan = run->nan != 0;
-            const float unit = cut ? run->vmax : run->vmax / l;
+            const bool nan = nans[run & (kTileSlots - 1)] != 0;
+            const float unit = cut ? ref : ref / l;
             if (busy) {
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
@@ -323,104 +343,144 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         // ---- conversion: codes to half precision, in the layout of the products ----
         constexpr int kLanes = D / 16, kAtOnce = 128 / kLanes, kIter = 128 / kAtOnce;   // 16 codes a lane; keys at once
         const int tid = threadIdx.x - 256, sub = tid & (kLanes - 1), key = tid / kLanes;
-        float* most = reinterpret_cast<float*>(smem + L::kMax);
         uint32_t done = 0;                                   // key tiles converted so far
-        int slot = 0;
-        const int shift = a.shape.page_shift, inside = a.shape.page - 1;
-        while (walk.next(a, r)) {
-            const int end = r.len + r.tokens;                // slots at or beyond it are not read
-            int id[kIter];
-            auto look = [&](int kt) {
+        int run = 0;
+        auto read = [&](int raw, int full, int free_, uint4 (&x)[kIter]) {       // a side's codes from their stage, which is free after that
+            const uint32_t st = done % L::kRaw, phase = done / L::kRaw & 1;
+            wait(full + st, phase);
+            const unsigned char* from = smem + raw + st * L::kCodes + tid * 16;
 #pragma unroll
-                for (int i = 0; i < kIter; ++i) {
-                    const int s = kt * kTileKeys + i * kAtOnce + key;
-                    id[i] = s < end ? max(0, kv_page(a.shape, a.table, r.b, s >> shift, a.status)) : -1;
-                }
-            };
-            auto load = [&](const uint8_t* side, const float* scales, int kt, uint4 (&x)[kIter], float (&sc)[kIter]) {
+            for (int i = 0; i < kIter; ++i) x[i] = *reinterpret_cast<const uint4*>(from + i * 2048);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + free_ + st);
+        };
+        auto write = [&](unsigned char* to, const uint4 (&x)[kIter], const uint32_t (&ratio)[8]) {
 #pragma unroll
-                for (int i = 0; i < kIter; ++i) {
-                    x[i] = make_uint4(0, 0, 0, 0);
-                    sc[i] = 0.f;
-                    if (id[i] >= 0) {
-                        const int s = kt * kTileKeys + i * kAtOnce + key;
-                        const long long head = (long long)id[i] * a.shape.kv_heads + r.h;
-                        x[i] = ld_nc_v4(reinterpret_cast<const uint4*>(side + (head * a.shape.page + (s & inside)) * D + sub * 16));
-                        sc[i] = __ldg(scales + head);
-                    }
+            for (int i = 0; i < kIter; ++i) {
+                const int row = i * kAtOnce + key;
+                const uint32_t two_f = ratio[row >> 4];
+                const __half2 f = *reinterpret_cast<const __half2*>(&two_f);
+                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                uint32_t h[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t two = from_e4m3x2((uint16_t)(w[e >> 1] >> (e & 1) * 16));
+                    const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&two), f);
+                    h[e] = *reinterpret_cast<const uint32_t*>(&y);
                 }
-            };
-            uint4 kx[kIter], vx[kIter];
-            float ksc[kIter], vsc[kIter];
-            look(r.k0);
-            load(a.kc, a.ks, r.k0, kx, ksc);
-            // the largest scales of the run's pages
-            float kmax = 0.f, vmax = 0.f;
-            const int p1 = (min(end, r.k1 * kTileKeys) - 1) >> shift;
-            for (int p = (r.k0 * kTileKeys >> shift) + tid; p <= p1; p += 128) {
-                const long long head = (long long)max(0, kv_page(a.shape, a.table, r.b, p, a.status)) * a.shape.kv_heads + r.h;
-                kmax = fmaxf(kmax, __ldg(a.ks + head)); vmax = fmaxf(vmax, __ldg(a.vs + head));
+                // two chunks of eight elements; lanes of the second 64 elements begin with the other one, whose banks are free
+                const int block = sub >> 2, chunk = (sub & 3) * 2;
+                unsigned char* base = to + block * (128 * 128) + row * 128;
+                const uint4 c0 = make_uint4(h[0], h[1], h[2], h[3]), c1 = make_uint4(h[4], h[5], h[6], h[7]);
+                *reinterpret_cast<uint4*>(base + (((chunk + block) ^ (row & 7)) << 4)) = block ? c1 : c0;
+                *reinterpret_cast<uint4*>(base + (((chunk + 1 - block) ^ (row & 7)) << 4)) = block ? c0 : c1;
             }
-            kmax = warp_max_f32(kmax); vmax = warp_max_f32(vmax);
-            if (lane == 0) { most[(warp - 8) * 2] = kmax; most[(warp - 8) * 2 + 1] = vmax; }
-            asm volatile("bar.sync 3, 128;" ::: "memory");
-#pragma unroll
-            for (int w = 0; w < 4; ++w) { kmax = fmaxf(kmax, most[w * 2]); vmax = fmaxf(vmax, most[w * 2 + 1]); }
-            asm volatile("bar.sync 3, 128;" ::: "memory");
-            TileRun* run = runs + slot;
-            slot = (slot + 1) & (kTileRunSlots - 1);
-            const float kinv = 1.f / kmax, vinv = 1.f / vmax;
-            auto write = [&](unsigned char* to, const uint4 (&x)[kIter], const float (&sc)[kIter], float inv) {
-#pragma unroll
-                for (int i = 0; i < kIter; ++i) {
-                    const int row = i * kAtOnce + key;
-                    const __half2 f = __float2half2_rn(sc[i] * inv);
-                    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                    uint32_t h[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t two = from_e4m3x2((uint16_t)(w[e >> 1] >> (e & 1) * 16));
-                        const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&two), f);
-                        h[e] = *reinterpret_cast<const uint32_t*>(&y);
-                    }
-                    // two chunks of eight elements; lanes of the second 64 elements begin with the other one, whose banks are free
-                    const int block = sub >> 2, chunk = (sub & 3) * 2;
-                    unsigned char* base = to + block * (128 * 128) + row * 128;
-                    const uint4 c0 = make_uint4(h[0], h[1], h[2], h[3]), c1 = make_uint4(h[4], h[5], h[6], h[7]);
-                    *reinterpret_cast<uint4*>(base + (((chunk + block) ^ (row & 7)) << 4)) = block ? c1 : c0;
-                    *reinterpret_cast<uint4*>(base + (((chunk + 1 - block) ^ (row & 7)) << 4)) = block ? c0 : c1;
-                }
-            };
+        };
+        while (walk.next(a, r)) {
+            const int end = r.len + r.tokens;                // slots at or beyond it are not the sequence's
             for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
                 const uint32_t stage = done & 1, phase = done >> 1 & 1;
-                load(a.vc, a.vs, kt, vx, vsc);
+                const TileInfo& info = infos[done & (kTileSlots - 1)];
+                uint4 x[kIter];
+                read(L::kRawK, L::kBarRKFull, L::kBarRKFree, x);
                 wait(L::kBarKFree + stage, phase ^ 1);
-                if (kt == r.k0) {                            // the slot's last run is over (see kTileRunSlots)
-                    if (tid == 0) { run->kmax = kmax; run->vmax = vmax; run->nan = 0; }
-                    asm volatile("bar.sync 3, 128;" ::: "memory");
-                }
-                write(smem + L::kK + stage * L::kOperand, kx, ksc, kinv);
+                write(smem + L::kK + stage * L::kOperand, x, info.kratio);
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + L::kBarKFull + stage);
-                if (kt + 1 < r.k1) { look(kt + 1); load(a.kc, a.ks, kt + 1, kx, ksc); }
-                if ((kt + 1) * kTileKeys > r.len) {          // NaN codes of the step's own values
+                read(L::kRawV, L::kBarRVFull, L::kBarRVFree, x);
+                if ((kt + 1) * kTileKeys > r.len) {          // NaN codes of the step's own values, and what lies behind them
                     uint32_t seen = 0;
 #pragma unroll
-                    for (int i = 0; i < kIter; ++i)
-                        if (kt * kTileKeys + i * kAtOnce + key >= r.len) {
-                            vx[i].x = drop_nan(vx[i].x, seen); vx[i].y = drop_nan(vx[i].y, seen);
-                            vx[i].z = drop_nan(vx[i].z, seen); vx[i].w = drop_nan(vx[i].w, seen);
+                    for (int i = 0; i < kIter; ++i) {
+                        const int s = kt * kTileKeys + i * kAtOnce + key;
+                        if (s >= end) x[i] = make_uint4(0, 0, 0, 0);
+                        else if (s >= r.len) {
+                            x[i].x = drop_nan(x[i].x, seen); x[i].y = drop_nan(x[i].y, seen);
+                            x[i].z = drop_nan(x[i].z, seen); x[i].w = drop_nan(x[i].w, seen);
                         }
-                    if (seen) atomicOr(&run->nan, 1);
+                    }
+                    if (seen) atomicOr(nans + (run & (kTileSlots - 1)), 1);
                 }
                 wait(L::kBarVFree + stage, phase ^ 1);
-                write(smem + L::kV + stage * L::kOperand, vx, vsc, vinv);
+                write(smem + L::kV + stage * L::kOperand, x, info.vratio);
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + L::kBarVFull + stage);
             }
+            ++run;
         }
+    } else if (warp == 13) {
+        // ---- copies: pages of a key tile, a lane for each 16 keys; four tiles are looked up at a time, four ahead ----
+        uint32_t done = 0;
+        int run = 0;
+        const int shift = a.shape.page_shift, inside = a.shape.page - 1;
+        const int copy_rows = min(a.shape.page, kTileKeys);
+        while (walk.next(a, r)) {
+            const int end = r.len + r.tokens;
+            int id[2];
+            float ks[2], vs[2];
+            auto look = [&](int batch, int& i, float& k, float& v) {
+                const int s = (r.k0 + batch * 4) * kTileKeys + lane * 16;
+                i = -1; k = v = 0.f;
+                if (s < min(end, r.k1 * kTileKeys)) {
+                    i = max(0, kv_page(a.shape, a.table, r.b, s >> shift, a.status));
+                    const long long head = (long long)i * a.shape.kv_heads + r.h;
+                    k = __ldg(a.ks + head); v = __ldg(a.vs + head);
+                }
+            };
+            look(0, id[0], ks[0], vs[0]);
+            look(1, id[1], ks[1], vs[1]);
+            float ref = 0.f;
+            for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
+                const int n = kt - r.k0;
+                if (n && (n & 3) == 0) {
+                    id[0] = id[1]; ks[0] = ks[1]; vs[0] = vs[1];
+                    look((n >> 2) + 1, id[1], ks[1], vs[1]);
+                }
+                // lanes 0 to 7: this tile's groups of 16 keys
+                const int from = (n & 3) * 8 + (lane & 7);
+                const int mine = __shfl_sync(0xFFFFFFFFu, id[0], from);
+                const float k = __shfl_sync(0xFFFFFFFFu, ks[0], from), v = __shfl_sync(0xFFFFFFFFu, vs[0], from);
+                const float kmax = warp_max_f32(k), vmax = warp_max_f32(v);
+                float fade = 1.f;
+                if (n == 0) ref = vmax;
+                else if (vmax > 64.f * ref) { fade = ref / vmax; ref = vmax; }
+                const int s = kt * kTileKeys + lane * 16;
+                const bool copies = lane < 8 && mine >= 0 && (s & (copy_rows - 1)) == 0;
+                const uint32_t bytes = __popc(__ballot_sync(0xFFFFFFFFu, copies)) * copy_rows * D;
+                const uint32_t st = done % L::kRaw, phase = done / L::kRaw & 1;
+                const long long row = ((long long)mine * a.shape.kv_heads + r.h) * a.shape.page + (s & inside);
+                wait(L::kBarRKFree + st, phase ^ 1);
+                if (lane < 8) {
+                    TileInfo& info = infos[done & (kTileSlots - 1)];
+                    const __half2 kr = __float2half2_rn(kmax > 0.f ? k / kmax : 0.f), vr = __float2half2_rn(ref > 0.f ? v / ref : 0.f);
+                    info.kratio[lane] = *reinterpret_cast<const uint32_t*>(&kr);
+                    info.vratio[lane] = *reinterpret_cast<const uint32_t*>(&vr);
+                    if (lane == 0) {
+                        info.kmax = kmax; info.fade = fade; info.ref = ref;
+                        if (n == 0) nans[run & (kTileSlots - 1)] = 0;
+                    }
+                }
+                __syncwarp();
+                if (dead) continue;                          // (nobody takes codes any more)
+                if (lane == 0) mbar_expect_tx(bars + L::kBarRKFull + st, bytes);
+                __syncwarp();
+                if (copies) bulk_load(smem + L::kRawK + st * L::kCodes + lane * 16 * D, a.kc + row * D, copy_rows * D, bars + L::kBarRKFull + st);
+                wait(L::kBarRVFree + st, phase ^ 1);
+                if (dead) continue;
+                if (lane == 0) mbar_expect_tx(bars + L::kBarRVFull + st, bytes);
+                __syncwarp();
+                if (copies) bulk_load(smem + L::kRawV + st * L::kCodes + lane * 16 * D, a.vc + row * D, copy_rows * D, bars + L::kBarRVFull + st);
+            }
+            ++run;
+        }
+        // copies in flight land before the CTA ends, also where their reader has given up
+        for (uint32_t i = 0; i < L::kRaw; ++i)
+            if (dead && done > i) {
+                mbar_wait_warp(bars + L::kBarRKFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
+                mbar_wait_warp(bars + L::kBarRVFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
+            }
     } else {
         // ---- products: one lane issues ----
         constexpr uint32_t kScores = tc_idesc(kTileKeys, false), kOutputs = tc_idesc(D, true);
