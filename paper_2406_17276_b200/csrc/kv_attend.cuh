@@ -161,15 +161,21 @@ struct KvWalk {
 };
 
 // NaN codes of a step's values are taken as zero by the tensor-core kernels, which would otherwise spread them to rows that do not
-// see the token (0 * NaN); rows that do see it get their NaN here.  x: one output of row `token`, element d.
-__device__ __noinline__ float kv_with_nan(const KvAttend& a, const KvRun& r, int token, int d, int D, float x) {
+// see the token (0 * NaN); outputs that do see one are made NaN here, after they have been stored: elements [d, d + n) of query row
+// `row`.
+template <int D, class T>
+__device__ __noinline__ void kv_mark_nan(const KvAttend& a, const KvRun& r, int row, int d, int n) {
+    const int token = (int)a.by_group.div((unsigned)row), hq = r.h * a.group + row - token * a.group;
+    uint16_t* to = const_cast<uint16_t*>(a.out.data) + r.b * a.out.batch + token * a.out.token + hq * a.out.head;
+#pragma unroll 1
     for (int j = 0; j < r.tokens; ++j) {
         if (!kv_sees(a.step, r.b, token, j)) continue;
         const int s = r.len + j, id = max(0, kv_page(a.shape, a.table, r.b, s >> a.shape.page_shift, a.status));
-        const uint8_t c = a.vc[(((long long)id * a.shape.kv_heads + r.h) * a.shape.page + (s & (a.shape.page - 1))) * D + d];
-        if ((c & 0x7F) == 0x7F) return __int_as_float(0x7FC00000);
+        const uint8_t* v = a.vc + (((long long)id * a.shape.kv_heads + r.h) * a.shape.page + (s & (a.shape.page - 1))) * D;
+#pragma unroll 1
+        for (int e = d; e < d + n; ++e)
+            if ((v[e] & 0x7F) == 0x7F) to[e] = (uint16_t)from_float2<T>(__int_as_float(0x7FC00000), 0.f);
     }
-    return x;
 }
 // Clears NaN codes and reports them.
 __device__ __forceinline__ uint32_t drop_nan(uint32_t four, uint32_t& seen) {
@@ -184,12 +190,8 @@ template <int kRows, int D> __host__ __device__ constexpr int kv_part_floats() {
 
 // A row's outputs at elements [d, d + N) of query row `row` of the run (row tile included).
 template <int D, int N, class T>
-__device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int row, int d, float (&x)[N], bool nan) {
+__device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int row, int d, const float (&x)[N], bool nan) {
     const int token = (int)a.by_group.div((unsigned)row), hq = r.h * a.group + row - token * a.group;
-    if (nan) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = kv_with_nan(a, r, token, d + i, D, x[i]);
-    }
     uint16_t* to = const_cast<uint16_t*>(a.out.data) + r.b * a.out.batch + token * a.out.token + hq * a.out.head + d;
     uint32_t w[N / 2];
 #pragma unroll
@@ -207,6 +209,7 @@ __device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int 
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) *reinterpret_cast<uint32_t*>(to + 2 * i) = w[i];
     }
+    if (nan) kv_mark_nan<D, T>(a, r, row, d, N);
 }
 __device__ __forceinline__ void kv_store_lse(const KvAttend& a, const KvRun& r, int row, float m, float l) {
     if (!a.lse) return;

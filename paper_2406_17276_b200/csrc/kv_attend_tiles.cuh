@@ -25,7 +25,12 @@
 
 namespace ot {
 
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 14 * 32;
+// Registers a thread of each warpgroup; together they are what a block of four warpgroups is launched with (kRegsLaunch each, which the
+// host checks), or the warps that ask for more would wait for good.
+constexpr int kRegsLaunch = 128, kRegsSoftmax = 184, kRegsConvert = 80, kRegsIssue = 64;
+static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsIssue <= 4 * kRegsLaunch, "registers of a block");
+
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 16 * 32;
 
 // --- tcgen05 ---
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_word, uint32_t columns) {
@@ -50,18 +55,23 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, unsigned long 
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at, float (&x)[32]) {
-    uint32_t r[32];
+// 32 columns of this warp's lanes, to be used after tmem_wait (which names the registers, so that no use moves before it).
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&x)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
                  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-                   "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-                   "=r"(r[30]), "=r"(r[31])
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]),
+                 "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]),
+                 "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]),
+                 "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
                  : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_wait(float (&x)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]),
+                 "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]), "+f"(x[17]), "+f"(x[18]),
+                 "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]),
+                 "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31])
+                 :: "memory");
 }
 __device__ __forceinline__ void tmem_store32(uint32_t at, const float (&x)[32]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -92,9 +102,8 @@ __host__ __device__ constexpr uint32_t tc_idesc(int n, bool mn) { return 1u << 4
 // half precision).
 struct TileInfo {
     uint32_t kratio[8], vratio[8];       // of each 16 keys, twice in half precision
-    float kmax;
-    float fade, ref;                     // factor for the outputs so far, reference of the values
-    float pad;
+    float kmax, ref;                     // largest scale of the keys, reference of the values
+    float pad[2];
 };
 // Slots of TileInfo, by tile, and of the NaN word, by run.  The copying warp writes those of tile t (of run r) once the codes of tile t - 2 at
 // least have been taken; then values of t - 3 have been written, so the products of t - 5 are complete, so both softmax groups are done with
@@ -109,8 +118,8 @@ template <int D> struct TileLayout {
     enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 2,
            kBarO = kBarP + 2, kBarRKFull = kBarO + 2, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
            kBarEnd = kBarRVFree + kRaw, kBarCount };
-    static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4;
-    static constexpr int kBytes = kWord + 16 + 1024;         // the base is brought to a multiple of 1024
+    static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16;
+    static constexpr int kBytes = kMerge + 1024 + 1024;         // the base is brought to a multiple of 1024
     static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
 };
 static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
@@ -187,19 +196,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     if (!any) {
     } else if (warp < 8) {
         // ---- softmax: a thread a row ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int X = warp >> 2, in_tile = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) * 32u << 16);
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
-        uint32_t tiles = 0, outs = 0, runs_seen = 0, at = 0;     // at: key tiles of all runs, also those without rows for X
+        uint32_t tiles = 0, outs = 0, at = 0;                // at: key tiles of the runs before
+        int run = 0;
         while (walk.next(a, r)) {
-            const int row0 = r.rt * 2 * kTileRows + X * kTileRows, rows = min(kTileRows, r.tokens * a.group - row0);   // rows <= 0: none for X
+            const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
+            const int row0 = r.rt * 2 * kTileRows + (single ? 0 : X * kTileRows), rows = min(kTileRows, r.tokens * a.group - row0);
             const int row = row0 + in_tile;
             const bool mine = in_tile < rows, busy = (warp & 3) * 32 < rows;       // this thread, this warp
             const int token = (int)a.by_group.div((unsigned)min(row, r.tokens * a.group - 1));
             // queries to shared memory; bf16 rows are brought to half precision by a power of two of their own (exact but for
             // elements below 2^-22 of the row's largest)
             float qf = a.scale;
-            if (rows > 0) {
+            {
                 uint4 q[D / 8];
                 if (mine) {
                     const int hq = r.h * a.group + row - token * a.group;
@@ -223,108 +235,162 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     f = power_of_two(8 - e);
                     qf *= power_of_two(e - 8);
                 }
-                unsigned char* at = smem + L::kQ + X * L::kOperand + in_tile * 128;
+                if (!single || X == 0) {
+                    unsigned char* to_q = smem + L::kQ + X * L::kOperand + in_tile * 128;
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                    uint32_t h[4];
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                        uint32_t h[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 y = to_float2<T>(w[e]);
-                        h[e] = std::is_same<T, __half>::value ? w[e] : from_float2<__half>(y.x * f, y.y * f);
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 y = to_float2<T>(w[e]);
+                            h[e] = std::is_same<T, __half>::value ? w[e] : from_float2<__half>(y.x * f, y.y * f);
+                        }
+                        *reinterpret_cast<uint4*>(to_q + (i >> 3) * (128 * 128) + (((i & 7) ^ (in_tile & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                     }
-                    *reinterpret_cast<uint4*>(at + (i >> 3) * (128 * 128) + (((i & 7) ^ (in_tile & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                 }
             }
             proxy_fence();
             __syncwarp();
             if (lane == 0) mbar_arrive(bars + L::kBarQ);
-            const int run = (int)runs_seen++;
-            if (rows <= 0) {                                 // in step with the others: one arrival a run
-                wait(L::kBarQ, run & 1);
-                at += r.k1 - r.k0;
-                continue;
-            }
             float m = -INFINITY, l = 0.f, ref = 1.f;
-            for (int kt = r.k0; kt < r.k1; ++kt, ++tiles, ++at) {
+            const int first = r.k0 + (single ? X : 0), step = single ? 2 : 1;      // this group's key tiles
+            for (int kt = first; kt < r.k1; kt += step, ++tiles) {
                 wait(L::kBarS + X, tiles & 1);
                 tc_fence_after();
                 if (busy) {
-                    const TileInfo& info = infos[at & (kTileSlots - 1)];
-                    const float f = fmaxf(qf * info.kmax, 1.2e-38f), unit = info.fade;
+                    const TileInfo& info = infos[(at + kt - r.k0) & (kTileSlots - 1)];
+                    const float f = fmaxf(qf * info.kmax, 1.2e-38f);
+                    const float unit = ref == info.ref ? 1.f : ref / info.ref;
                     ref = info.ref;
-                    const int j0 = kt * kTileKeys - r.len;   // the tile's first slot, as a token of the step
-                    const bool edge = j0 + kTileKeys > 0;
-                    float x[32], top = -INFINITY;
+                    float x[4][32];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_load32(ts + c * 32, x);
-                        if (edge) {
+                    for (int c = 0; c < 4; ++c) tmem_load(ts + c * 32, x[c]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_wait(x[c]);
+                    const int j0 = kt * kTileKeys - r.len;   // the tile's first slot, as a token of the step
+                    if (j0 + kTileKeys > 0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
                             const uint32_t see = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = see >> i & 1 ? x[i] : -INFINITY;
+                            for (int i = 0; i < 32; ++i) x[c][i] = see >> i & 1 ? x[c][i] : -INFINITY;
                         }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i]);
                     }
-                    top *= f;
+                    float top4[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        top4[c] = x[c][0];
+#pragma unroll
+                        for (int i = 1; i < 32; ++i) top4[c] = fmaxf(top4[c], x[c][i]);
+                    }
+                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * f;
                     const float was = m;
                     const bool grows = top > m + (kLift + kGrowth);          // (the first score that is seen, too)
                     if (grows) m = top - kLift;
-                    if (kt > r.k0 && (unit != 1.f || __any_sync(0xFFFFFFFFu, grows))) {
+                    if (kt > first && (unit != 1.f || __any_sync(0xFFFFFFFFu, grows))) {
                         float fade = grows ? ex2_approx(was - m) : 1.f;
                         l *= fade;
                         fade *= unit;
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D / 32; ++c) {
-                            tmem_load32(to + c * 32, x);
+                            float o[32];
+                            tmem_load(to + c * 32, o);
+                            tmem_wait(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] *= fade;
-                            tmem_store32(to + c * 32, x);
+                            for (int i = 0; i < 32; ++i) o[i] *= fade;
+                            tmem_store32(to + c * 32, o);
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    float sum0 = 0.f, sum1 = 0.f;
+                    const unsigned long long f2 = pack2(f, f), base2 = pack2(-base, -base);
+                    unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tmem_load32(ts + c * 32, x);
-                        if (edge) {
-                            const uint32_t see = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = see >> i & 1 ? x[i] : -INFINITY;
-                        }
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float e0 = ex2_approx(fmaf(x[2 * i], f, -base)), e1 = ex2_approx(fmaf(x[2 * i + 1], f, -base));
-                            sum0 += e0; sum1 += e1;
+                            float e0, e1;
+                            unpack2(fma2(pack2(x[c][2 * i], x[c][2 * i + 1]), f2, base2), e0, e1);
+                            e0 = ex2_approx(e0); e1 = ex2_approx(e1);
+                            sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
                             p[i] = from_float2<__half>(e0, e1);
                         }
                         tmem_store16(ts + c * 16, p);
                     }
-                    l += sum0 + sum1;
+                    float s0, s1;
+                    unpack2(add2(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
                     tmem_wait_stores();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bars + L::kBarP + X);
             }
-            wait(L::kBarO + X, outs & 1);
-            ++outs;
+            at += r.k1 - r.k0;
+            const bool has = first < r.k1;                   // (a single row tile with one key tile has none for X = 1)
+            if (has) {
+                wait(L::kBarO + X, outs & 1);
+                ++outs;
+            }
             tc_fence_after();
             const bool cut = r.first != r.last;
             constexpr int kFloats = kv_part_floats<kTileRows, D>();
-            float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + X) * kFloats;
+            float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + (single ? 0 : X)) * kFloats;
             const bool nan = nans[run & (kTileSlots - 1)] != 0;
-            const float unit = cut ? ref : ref / l;
-            if (busy) {
+            ++run;
+            // a single row tile: the second group hands its sums to the first, over the queries, whose products are done
+            float mine_f = ref, other_f = 0.f;
+            float* hand = reinterpret_cast<float*>(smem + L::kQ);                  // [128][D], chunks of four swizzled by row
+            float* hand_ml = reinterpret_cast<float*>(smem + L::kMerge);           // [2][128]
+            if (single) {
+                if (X == 1) {
+                    if (mine && has) {
+                        hand_ml[in_tile] = m; hand_ml[128 + in_tile] = l;
+                    } else {
+                        hand_ml[in_tile] = -INFINITY; hand_ml[128 + in_tile] = 0.f;
+                    }
+                    if (busy && has) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            float o[32];
+                            tmem_load(to + c * 32, o);
+                            tmem_wait(o);
 #pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<float4*>(hand + in_tile * D + (((c * 8 + i) ^ (in_tile & (D / 4 - 1))) << 2)) =
+                                    make_float4(o[4 * i] * ref, o[4 * i + 1] * ref, o[4 * i + 2] * ref, o[4 * i + 3] * ref);
+                        }
+                    }
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (X == 0) {
+                    const float m1 = hand_ml[in_tile], mm = fmaxf(m, m1), base = mm == -INFINITY ? 0.f : mm;
+                    const float f0 = ex2_approx(m - base);
+                    other_f = ex2_approx(m1 - base);
+                    l = l * f0 + hand_ml[128 + in_tile] * other_f;
+                    mine_f = ref * f0;
+                    m = mm;
+                }
+            }
+            const float norm = cut ? 1.f : 1.f / l;
+            mine_f *= norm; other_f *= norm;
+            if (busy && (!single || X == 0)) {
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     float x[32];
-                    tmem_load32(to + c * 32, x);
+                    tmem_load(to + c * 32, x);
+                    tmem_wait(x);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] *= unit;
+                    for (int i = 0; i < 32; ++i) x[i] *= mine_f;
                     if (!mine) continue;
+                    if (single && r.k1 - r.k0 > 1) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 y = *reinterpret_cast<const float4*>(hand + in_tile * D + (((c * 8 + i) ^ (in_tile & (D / 4 - 1))) << 2));
+                            x[4 * i] += y.x * other_f; x[4 * i + 1] += y.y * other_f; x[4 * i + 2] += y.z * other_f; x[4 * i + 3] += y.w * other_f;
+                        }
+                    }
                     if (cut) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
@@ -335,12 +401,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 }
                 if (mine && cut) { part[kTileRows * D + in_tile] = m; part[kTileRows * D + kTileRows + in_tile] = l; }
                 if (mine && !cut) kv_store_lse(a, r, row, m, l);
+                if (cut && in_tile == 0) reinterpret_cast<int*>(part)[kTileRows * D + 2 * kTileRows] = nan;
             }
             tc_fence_before();
-            if (cut && in_tile == 0) reinterpret_cast<int*>(part)[kTileRows * D + 2 * kTileRows] = nan;
+            if (single) asm volatile("bar.sync 1, 256;" ::: "memory");             // the queries' place is free again
         }
     } else if (warp < 12) {
         // ---- conversion: codes to half precision, in the layout of the products ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         constexpr int kLanes = D / 16, kAtOnce = 128 / kLanes, kIter = 128 / kAtOnce;   // 16 codes a lane; keys at once
         const int tid = threadIdx.x - 256, sub = tid & (kLanes - 1), key = tid / kLanes;
         uint32_t done = 0;                                   // key tiles converted so far
@@ -410,7 +478,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
             ++run;
         }
-    } else if (warp == 13) {
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == 13) {
         // ---- copies: pages of a key tile, a lane for each 16 keys; four tiles are looked up at a time, four ahead ----
         uint32_t done = 0;
         int run = 0;
@@ -443,9 +513,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 const int mine = __shfl_sync(0xFFFFFFFFu, id[0], from);
                 const float k = __shfl_sync(0xFFFFFFFFu, ks[0], from), v = __shfl_sync(0xFFFFFFFFu, vs[0], from);
                 const float kmax = warp_max_f32(k), vmax = warp_max_f32(v);
-                float fade = 1.f;
-                if (n == 0) ref = vmax;
-                else if (vmax > 64.f * ref) { fade = ref / vmax; ref = vmax; }
+                if (n == 0 || vmax > 64.f * ref) ref = vmax;
                 const int s = kt * kTileKeys + lane * 16;
                 const bool copies = lane < 8 && mine >= 0 && (s & (copy_rows - 1)) == 0;
                 const uint32_t bytes = __popc(__ballot_sync(0xFFFFFFFFu, copies)) * copy_rows * D;
@@ -458,7 +526,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     info.kratio[lane] = *reinterpret_cast<const uint32_t*>(&kr);
                     info.vratio[lane] = *reinterpret_cast<const uint32_t*>(&vr);
                     if (lane == 0) {
-                        info.kmax = kmax; info.fade = fade; info.ref = ref;
+                        info.kmax = kmax; info.ref = ref;
                         if (n == 0) nans[run & (kTileSlots - 1)] = 0;
                     }
                 }
@@ -481,66 +549,89 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 mbar_wait_warp(bars + L::kBarRKFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
                 mbar_wait_warp(bars + L::kBarRVFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
             }
-    } else {
+    } else if (warp == 12) {
         // ---- products: one lane issues ----
         constexpr uint32_t kScores = tc_idesc(kTileKeys, false), kOutputs = tc_idesc(D, true);
         const uint32_t sq = smem_u32(smem + L::kQ), sk = smem_u32(smem + L::kK), sv = smem_u32(smem + L::kV);
         uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
-        auto scores = [&](int X, uint32_t stage) {
+        auto scores = [&](int X, int Q, uint32_t stage) {
             if (lane == 0) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k >> 2) * (128 * 128) + (k & 3) * 32;
-                    tc_mma_ss(tmem + L::kColS + X * 128, tc_desc(sq + X * L::kOperand + at, 16), tc_desc(sk + stage * L::kOperand + at, 16), kScores, k > 0);
+                    tc_mma_ss(tmem + L::kColS + X * 128, tc_desc(sq + Q * L::kOperand + at, 16), tc_desc(sk + stage * L::kOperand + at, 16), kScores, k > 0);
                 }
                 tc_commit(bars + L::kBarS + X);
             }
             __syncwarp();
         };
+        auto outputs = [&](int X, uint32_t stage, bool add, bool last) {
+            wait(L::kBarP + X, tiles[X] & 1);
+            ++tiles[X];
+            tc_fence_after();
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < kTileKeys / 16; ++k)
+                    tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + k * 8, tc_desc(sv + stage * L::kOperand + k * 2048, 128 * 128), kOutputs, add || k > 0);
+                if (last) tc_commit(bars + L::kBarO + X);
+            }
+            __syncwarp();
+        };
+        auto keys = [&](uint32_t tile) {                     // waits for a tile's keys
+            wait(L::kBarKFull + (tile & 1), tile >> 1 & 1);
+            tc_fence_after();
+        };
+        auto commit = [&](int bar) {
+            if (lane == 0) tc_commit(bars + bar);
+            __syncwarp();
+        };
         while (walk.next(a, r)) {
-            const int left = r.tokens * a.group - r.rt * 2 * kTileRows;
-            const int X1 = left > kTileRows ? 2 : 1;
+            const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
+            const int n = r.k1 - r.k0;
             wait(L::kBarQ, nrun & 1);
             ++nrun;
-            wait(L::kBarKFull + (done & 1), done >> 1 & 1);
-            tc_fence_after();
-            for (int X = 0; X < X1; ++X) scores(X, done & 1);
-            if (lane == 0) tc_commit(bars + L::kBarKFree + (done & 1));
-            for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
-                const uint32_t stage = done & 1, next = (done + 1) & 1;
-                const bool more = kt + 1 < r.k1;
-                wait(L::kBarVFull + stage, done >> 1 & 1);
-                for (int X = 0; X < X1; ++X) {
-                    wait(L::kBarP + X, tiles[X] & 1);
-                    ++tiles[X];
-                    tc_fence_after();
-                    if (lane == 0) {
-#pragma unroll
-                        for (int k = 0; k < kTileKeys / 16; ++k)
-                            tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + k * 8, tc_desc(sv + stage * L::kOperand + k * 2048, 128 * 128), kOutputs,
-                                      kt > r.k0 || k > 0);
-                        if (!more) tc_commit(bars + L::kBarO + X);
+            if (single) {                                    // one row tile: the two groups take its key tiles in turn
+                for (int i = 0; i < min(n, 2); ++i) {
+                    keys(done + i);
+                    scores(i, 0, (done + i) & 1);
+                    commit(L::kBarKFree + ((done + i) & 1));
+                }
+                for (int i = 0; i < n; ++i, ++done) {
+                    const uint32_t stage = done & 1;
+                    wait(L::kBarVFull + stage, done >> 1 & 1);
+                    outputs(i & 1, stage, i > 1, i + 2 >= n);
+                    commit(L::kBarVFree + stage);
+                    if (i + 2 < n) {
+                        keys(done + 2);
+                        scores(i & 1, 0, stage);
+                        commit(L::kBarKFree + stage);
                     }
-                    __syncwarp();
-                    if (more) {
-                        if (X == 0) {
-                            wait(L::kBarKFull + next, (done + 1) >> 1 & 1);
-                            tc_fence_after();
+                }
+            } else {                                         // two row tiles in turn
+                keys(done);
+                for (int X = 0; X < 2; ++X) scores(X, X, done & 1);
+                commit(L::kBarKFree + (done & 1));
+                for (int i = 0; i < n; ++i, ++done) {
+                    const uint32_t stage = done & 1, next = (done + 1) & 1;
+                    const bool more = i + 1 < n;
+                    wait(L::kBarVFull + stage, done >> 1 & 1);
+                    for (int X = 0; X < 2; ++X) {
+                        outputs(X, stage, i > 0, !more);
+                        if (more) {
+                            if (X == 0) keys(done + 1);
+                            scores(X, X, next);
                         }
-                        scores(X, next);
                     }
+                    commit(L::kBarVFree + stage);
+                    if (more) commit(L::kBarKFree + next);
                 }
-                if (lane == 0) {
-                    tc_commit(bars + L::kBarVFree + stage);
-                    if (more) tc_commit(bars + L::kBarKFree + next);
-                }
-                __syncwarp();
             }
         }
         // everything issued is complete before TMEM is given back, also after a wait that ran out
         if (lane == 0) tc_commit(bars + L::kBarEnd);
         __syncwarp();
         mbar_wait_warp(bars + L::kBarEnd, 0, a.status);
+    }
     }
     tc_fence_before();
     __syncthreads();
