@@ -86,6 +86,13 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16
                  ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]),
                    "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
 }
+// One lane of a converged warp, always the same one.  (Asked by elect.sync and not by the lane's number, the compiler knows that a single
+// thread is left, and hands the tensor instructions their operands without asking every lane for its own.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
 __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Shared-memory descriptor of a 128-byte-swizzled operand: rows of 128 bytes, eight rows an atom of 1024 bytes.  Along the summed index (K-major)
@@ -555,7 +562,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         const uint32_t sq = smem_u32(smem + L::kQ), sk = smem_u32(smem + L::kK), sv = smem_u32(smem + L::kV);
         uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
         auto scores = [&](int X, int Q, uint32_t stage) {
-            if (lane == 0) {
+            if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k >> 2) * (128 * 128) + (k & 3) * 32;
@@ -569,7 +576,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             wait(L::kBarP + X, tiles[X] & 1);
             ++tiles[X];
             tc_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < kTileKeys / 16; ++k)
                     tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + k * 8, tc_desc(sv + stage * L::kOperand + k * 2048, 128 * 128), kOutputs, add || k > 0);
@@ -582,7 +589,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             tc_fence_after();
         };
         auto commit = [&](int bar) {
-            if (lane == 0) tc_commit(bars + bar);
+            if (elect_one()) tc_commit(bars + bar);
             __syncwarp();
         };
         while (walk.next(a, r)) {
@@ -628,7 +635,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
         }
         // everything issued is complete before TMEM is given back, also after a wait that ran out
-        if (lane == 0) tc_commit(bars + L::kBarEnd);
+        if (elect_one()) tc_commit(bars + L::kBarEnd);
         __syncwarp();
         mbar_wait_warp(bars + L::kBarEnd, 0, a.status);
     }
