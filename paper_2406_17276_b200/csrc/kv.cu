@@ -141,9 +141,7 @@ int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
     }
     for (int rows : kVariantRows) {
         const AttendVariant v = attend_for(*cfg, rows);
-        cudaFuncAttributes got;
-        if (cudaFuncGetAttributes(&got, v.kernel) != cudaSuccess || (v.join && got.numRegs != ot::kRegsLaunch) ||
-            cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem) != cudaSuccess) {
             cudaGetLastError();
             cudaFree(kv->base);
             delete kv;

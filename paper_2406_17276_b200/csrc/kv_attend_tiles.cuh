@@ -14,9 +14,9 @@
 //   q          softmax -> products      queries of a run are in shared memory
 //   rk, rv     copies <-> conversion    codes of a key tile
 //   k, v       conversion <-> products  operands, two stages each
-//   s[X]       products -> softmax X    scores of a key tile; all earlier products of X are complete, so O may be rescaled
-//   p[X]       softmax X -> products
-//   o[X]       products -> softmax X    the run's last product
+//   s[X][2]    products -> softmax X    scores of half a key tile: one half's are ready while the other's exponentials are taken
+//   p[X][2]    softmax X -> products
+//   o[X][2]    products -> softmax X    O holds the values of half a key tile (waited for before O is rescaled, and at the end)
 #pragma once
 
 #include <type_traits>
@@ -25,12 +25,7 @@
 
 namespace ot {
 
-// Registers a thread of each warpgroup; together they are what a block of four warpgroups is launched with (kRegsLaunch each, which the
-// host checks), or the warps that ask for more would wait for good.
-constexpr int kRegsLaunch = 128, kRegsSoftmax = 184, kRegsConvert = 80, kRegsIssue = 64;
-static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsIssue <= 4 * kRegsLaunch, "registers of a block");
-
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 16 * 32;
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 14 * 32;
 
 // --- tcgen05 ---
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_word, uint32_t columns) {
@@ -122,8 +117,8 @@ template <int D> struct TileLayout {
     static constexpr int kCodes = 128 * D, kRaw = D == 128 ? 1 : 2;          // codes of one side of a key tile; stages of them
     static constexpr int kQ = 0, kK = 2 * kOperand, kV = kK + 2 * kOperand, kRawK = kV + 2 * kOperand, kRawV = kRawK + kRaw * kCodes;
     static constexpr int kBars = kRawV + kRaw * kCodes;
-    enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 2,
-           kBarO = kBarP + 2, kBarRKFull = kBarO + 2, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
+    enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 4,
+           kBarO = kBarP + 4, kBarRKFull = kBarO + 4, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
            kBarEnd = kBarRVFree + kRaw, kBarCount };
     static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16;
     static constexpr int kBytes = kMerge + 1024 + 1024;         // the base is brought to a multiple of 1024
@@ -160,6 +155,11 @@ __device__ __forceinline__ uint32_t kv_sees32(const KvStep& st, int b, int i, in
 // of the largest; relative to the largest alone, small ones would lose bits that matter where the large ones' values cancel).
 constexpr float kLift = 10.f, kGrowth = 5.f;
 
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {         // NaN if any is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 template <int D, class T>
 __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const __grid_constant__ KvAttend a) {
     using L = TileLayout<D>;
@@ -176,7 +176,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             for (int i = 0; i < 2; ++i) {
                 mbar_init(bars + L::kBarKFull + i, 4); mbar_init(bars + L::kBarKFree + i, 1);
                 mbar_init(bars + L::kBarVFull + i, 4); mbar_init(bars + L::kBarVFree + i, 1);
-                mbar_init(bars + L::kBarS + i, 1); mbar_init(bars + L::kBarP + i, 4); mbar_init(bars + L::kBarO + i, 1);
+                for (int k = 0; k < 2; ++k) {
+                    mbar_init(bars + L::kBarS + 2 * i + k, 1); mbar_init(bars + L::kBarP + 2 * i + k, 4); mbar_init(bars + L::kBarO + 2 * i + k, 1);
+                }
             }
             for (int i = 0; i < L::kRaw; ++i) {
                 mbar_init(bars + L::kBarRKFull + i, 1); mbar_init(bars + L::kBarRKFree + i, 4);
@@ -203,11 +205,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     if (!any) {
     } else if (warp < 8) {
         // ---- softmax: a thread a row ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int X = warp >> 2, in_tile = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) * 32u << 16);
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
-        uint32_t tiles = 0, outs = 0, at = 0;                // at: key tiles of the runs before
+        uint32_t tiles = 0, at = 0;                          // key tiles of this group, and of the runs before
         int run = 0;
         while (walk.next(a, r)) {
             const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
@@ -263,82 +264,95 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             float m = -INFINITY, l = 0.f, ref = 1.f;
             const int first = r.k0 + (single ? X : 0), step = single ? 2 : 1;      // this group's key tiles
             for (int kt = first; kt < r.k1; kt += step, ++tiles) {
-                wait(L::kBarS + X, tiles & 1);
-                tc_fence_after();
-                if (busy) {
-                    const TileInfo& info = infos[(at + kt - r.k0) & (kTileSlots - 1)];
-                    const float f = fmaxf(qf * info.kmax, 1.2e-38f);
-                    const float unit = ref == info.ref ? 1.f : ref / info.ref;
-                    ref = info.ref;
-                    float x[4][32];
+                const TileInfo& info = infos[(at + kt - r.k0) & (kTileSlots - 1)];
+                for (int half = 0; half < 2; ++half) {
+                    const int j0 = kt * kTileKeys + half * 64 - r.len;             // the first slot, as a token of the step
+                    const bool edge = j0 + 64 > 0;
+                    uint32_t see[2] = {0, 0};
+                    if (edge && busy) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_load(ts + c * 32, x[c]);
+                        for (int c = 0; c < 2; ++c) see[c] = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
+                    }
+                    wait(L::kBarS + 2 * X + half, tiles & 1);
+                    tc_fence_after();
+                    if (busy) {
+                        const uint32_t from = ts + half * 64;
+                        const float f = fmaxf(qf * info.kmax, 1.2e-38f);
+                        const float unit = ref == info.ref ? 1.f : ref / info.ref;
+                        ref = info.ref;
+                        float x[2][32];
+                        tmem_load(from, x[0]);
+                        tmem_load(from + 32, x[1]);
+                        tmem_wait(x[0]);
+                        tmem_wait(x[1]);
+                        if (edge) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_wait(x[c]);
-                    const int j0 = kt * kTileKeys - r.len;   // the tile's first slot, as a token of the step
-                    if (j0 + kTileKeys > 0) {
+                            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) x[c][i] = see[c] >> i & 1 ? x[c][i] : -INFINITY;
+                        }
+                        float top4[4];
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t see = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
+                            const float* y = x[c >> 1] + (c & 1) * 16;
+                            top4[c] = max3_nan(y[0], y[1], y[2]);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[c][i] = see >> i & 1 ? x[c][i] : -INFINITY;
+                            for (int i = 3; i < 15; i += 2) top4[c] = max3_nan(top4[c], y[i], y[i + 1]);
+                            top4[c] = max3_nan(top4[c], y[15], y[15]);
                         }
-                    }
-                    float top4[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        top4[c] = x[c][0];
-#pragma unroll
-                        for (int i = 1; i < 32; ++i) top4[c] = fmaxf(top4[c], x[c][i]);
-                    }
-                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * f;
-                    const float was = m;
-                    const bool grows = top > m + (kLift + kGrowth);          // (the first score that is seen, too)
-                    if (grows) m = top - kLift;
-                    if (kt > first && (unit != 1.f || __any_sync(0xFFFFFFFFu, grows))) {
-                        float fade = grows ? ex2_approx(was - m) : 1.f;
-                        l *= fade;
-                        fade *= unit;
+                        const float top = max3_nan(max3_nan(top4[0], top4[1], top4[2]), top4[3], top4[3]) * f;
+                        const float was = m;
+                        const bool grows = top > m + (kLift + kGrowth);      // (the first score that is seen, too)
+                        if (grows) m = top - kLift;
+                        if ((kt > first || half) && (unit != 1.f || __any_sync(0xFFFFFFFFu, grows))) {
+                            // S being there, the products of two halves ago are complete; those of the half before are waited for
+                            wait(L::kBarO + 2 * X + (half ^ 1), half ? tiles & 1 : (tiles - 1) & 1);
+                            tc_fence_after();
+                            float fade = grows ? ex2_approx(was - m) : 1.f;
+                            l *= fade;
+                            fade *= unit;
 #pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            float o[32];
-                            tmem_load(to + c * 32, o);
-                            tmem_wait(o);
+                            for (int c = 0; c < D / 32; ++c) {
+                                float o[32];
+                                tmem_load(to + c * 32, o);
+                                tmem_wait(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] *= fade;
-                            tmem_store32(to + c * 32, o);
+                                for (int i = 0; i < 32; ++i) o[i] *= fade;
+                                tmem_store32(to + c * 32, o);
+                            }
                         }
-                    }
-                    const float base = m == -INFINITY ? 0.f : m;
-                    const unsigned long long f2 = pack2(f, f), base2 = pack2(-base, -base);
-                    unsigned long long sum[2] = {0ull, 0ull};
+                        // a row that sees a NaN or an infinite score is NaN
+                        const float base = !(top < INFINITY) ? __int_as_float(0x7FC00000) : (m == -INFINITY ? 0.f : m);
+                        const unsigned long long f2 = pack2(f, f), base2 = pack2(-base, -base);
+                        unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t p[16];
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t p[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float e0, e1;
-                            unpack2(fma2(pack2(x[c][2 * i], x[c][2 * i + 1]), f2, base2), e0, e1);
-                            e0 = ex2_approx(e0); e1 = ex2_approx(e1);
-                            sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
-                            p[i] = from_float2<__half>(e0, e1);
+                            for (int i = 0; i < 16; ++i) {
+                                float e0, e1;
+                                unpack2(fma2(pack2(x[c][2 * i], x[c][2 * i + 1]), f2, base2), e0, e1);
+                                e0 = ex2_approx(e0); e1 = ex2_approx(e1);
+                                sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+                                p[i] = from_float2<__half>(e0, e1);
+                            }
+                            tmem_store16(from + c * 16, p);
                         }
-                        tmem_store16(ts + c * 16, p);
+                        float s0, s1;
+                        unpack2(add2(sum[0], sum[1]), s0, s1);
+                        l += s0 + s1;
+                        tmem_wait_stores();
                     }
-                    float s0, s1;
-                    unpack2(add2(sum[0], sum[1]), s0, s1);
-                    l += s0 + s1;
-                    tmem_wait_stores();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bars + L::kBarP + 2 * X + half);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + L::kBarP + X);
             }
             at += r.k1 - r.k0;
             const bool has = first < r.k1;                   // (a single row tile with one key tile has none for X = 1)
             if (has) {
-                wait(L::kBarO + X, outs & 1);
-                ++outs;
+                wait(L::kBarO + 2 * X, (tiles - 1) & 1);
+                wait(L::kBarO + 2 * X + 1, (tiles - 1) & 1);
             }
             tc_fence_after();
             const bool cut = r.first != r.last;
@@ -415,7 +429,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         }
     } else if (warp < 12) {
         // ---- conversion: codes to half precision, in the layout of the products ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         constexpr int kLanes = D / 16, kAtOnce = 128 / kLanes, kIter = 128 / kAtOnce;   // 16 codes a lane; keys at once
         const int tid = threadIdx.x - 256, sub = tid & (kLanes - 1), key = tid / kLanes;
         uint32_t done = 0;                                   // key tiles converted so far
@@ -485,9 +498,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
             ++run;
         }
-    } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
-    if (warp == 13) {
+    } else if (warp == 13) {
         // ---- copies: pages of a key tile, a lane for each 16 keys; four tiles are looked up at a time, four ahead ----
         uint32_t done = 0;
         int run = 0;
@@ -558,29 +569,31 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
     } else if (warp == 12) {
         // ---- products: one lane issues ----
-        constexpr uint32_t kScores = tc_idesc(kTileKeys, false), kOutputs = tc_idesc(D, true);
+        constexpr uint32_t kScores = tc_idesc(64, false), kOutputs = tc_idesc(D, true);
         const uint32_t sq = smem_u32(smem + L::kQ), sk = smem_u32(smem + L::kK), sv = smem_u32(smem + L::kV);
         uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
-        auto scores = [&](int X, int Q, uint32_t stage) {
+        auto scores = [&](int X, int Q, uint32_t stage, int half) {
             if (elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k >> 2) * (128 * 128) + (k & 3) * 32;
-                    tc_mma_ss(tmem + L::kColS + X * 128, tc_desc(sq + Q * L::kOperand + at, 16), tc_desc(sk + stage * L::kOperand + at, 16), kScores, k > 0);
+                    tc_mma_ss(tmem + L::kColS + X * 128 + half * 64, tc_desc(sq + Q * L::kOperand + at, 16),
+                              tc_desc(sk + stage * L::kOperand + half * (64 * 128) + at, 16), kScores, k > 0);
                 }
-                tc_commit(bars + L::kBarS + X);
+                tc_commit(bars + L::kBarS + 2 * X + half);
             }
             __syncwarp();
         };
-        auto outputs = [&](int X, uint32_t stage, bool add, bool last) {
-            wait(L::kBarP + X, tiles[X] & 1);
-            ++tiles[X];
+        auto outputs = [&](int X, uint32_t stage, int half, bool add) {
+            wait(L::kBarP + 2 * X + half, tiles[X] & 1);
+            tiles[X] += half;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < kTileKeys / 16; ++k)
-                    tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + k * 8, tc_desc(sv + stage * L::kOperand + k * 2048, 128 * 128), kOutputs, add || k > 0);
-                if (last) tc_commit(bars + L::kBarO + X);
+                for (int k = 0; k < 4; ++k)
+                    tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + half * 64 + k * 8,
+                              tc_desc(sv + stage * L::kOperand + half * (64 * 128) + k * 2048, 128 * 128), kOutputs, add || k > 0);
+                tc_commit(bars + L::kBarO + 2 * X + half);
             }
             __syncwarp();
         };
@@ -600,35 +613,39 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             if (single) {                                    // one row tile: the two groups take its key tiles in turn
                 for (int i = 0; i < min(n, 2); ++i) {
                     keys(done + i);
-                    scores(i, 0, (done + i) & 1);
+                    for (int half = 0; half < 2; ++half) scores(i, 0, (done + i) & 1, half);
                     commit(L::kBarKFree + ((done + i) & 1));
                 }
                 for (int i = 0; i < n; ++i, ++done) {
                     const uint32_t stage = done & 1;
                     wait(L::kBarVFull + stage, done >> 1 & 1);
-                    outputs(i & 1, stage, i > 1, i + 2 >= n);
-                    commit(L::kBarVFree + stage);
-                    if (i + 2 < n) {
-                        keys(done + 2);
-                        scores(i & 1, 0, stage);
-                        commit(L::kBarKFree + stage);
+                    for (int half = 0; half < 2; ++half) {
+                        outputs(i & 1, stage, half, i > 1 || half);
+                        if (i + 2 < n) {
+                            if (half == 0) keys(done + 2);
+                            scores(i & 1, 0, stage, half);
+                        }
                     }
+                    commit(L::kBarVFree + stage);
+                    if (i + 2 < n) commit(L::kBarKFree + stage);
                 }
             } else {                                         // two row tiles in turn
                 keys(done);
-                for (int X = 0; X < 2; ++X) scores(X, X, done & 1);
+                for (int half = 0; half < 2; ++half)
+                    for (int X = 0; X < 2; ++X) scores(X, X, done & 1, half);
                 commit(L::kBarKFree + (done & 1));
                 for (int i = 0; i < n; ++i, ++done) {
                     const uint32_t stage = done & 1, next = (done + 1) & 1;
                     const bool more = i + 1 < n;
                     wait(L::kBarVFull + stage, done >> 1 & 1);
-                    for (int X = 0; X < 2; ++X) {
-                        outputs(X, stage, i > 0, !more);
-                        if (more) {
-                            if (X == 0) keys(done + 1);
-                            scores(X, X, next);
+                    for (int half = 0; half < 2; ++half)
+                        for (int X = 0; X < 2; ++X) {
+                            outputs(X, stage, half, i > 0 || half);
+                            if (more) {
+                                if (X == 0 && half == 0) keys(done + 1);
+                                scores(X, X, next, half);
+                            }
                         }
-                    }
                     commit(L::kBarVFree + stage);
                     if (more) commit(L::kBarKFree + next);
                 }
@@ -638,7 +655,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         if (elect_one()) tc_commit(bars + L::kBarEnd);
         __syncwarp();
         mbar_wait_warp(bars + L::kBarEnd, 0, a.status);
-    }
     }
     tc_fence_before();
     __syncthreads();
