@@ -40,15 +40,21 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(unsigned long long* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, unsigned long long a, unsigned long long b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// Shared-memory descriptor of a 128-byte-swizzled operand: rows of 128 bytes, eight rows an atom of 1024 bytes.  Along the summed index (K-major)
+// or along the other (MN-major, with `block` bytes from one 64-element block of the other index to the next).  The address is in
+// the low word, the constant rest in the high one.
+__device__ __forceinline__ uint32_t tc_desc(uint32_t smem_address, uint32_t block) { return smem_address >> 4 | (block >> 4) << 16; }
+constexpr uint32_t kDescHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+// D (+)= A B, one step of 16 along the summed index.  A from shared memory, and from tensor memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "n"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, unsigned long long b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "n"(kDescHigh) : "memory");
 }
 // 32 columns of this warp's lanes, to be used after tmem_wait (which names the registers, so that no use moves before it).
 __device__ __forceinline__ void tmem_load(uint32_t at, float (&x)[32]) {
@@ -90,12 +96,6 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Shared-memory descriptor of a 128-byte-swizzled operand: rows of 128 bytes, eight rows an atom of 1024 bytes.  Along the summed index (K-major)
-// or along the other (MN-major); `block`: bytes from one 64-element block of the other index to the next (MN-major only).
-__device__ __forceinline__ unsigned long long tc_desc(uint32_t smem_address, uint32_t block) {
-    return (unsigned long long)(smem_address >> 4 & 0x3FFF) | (unsigned long long)(block >> 4) << 16 | (unsigned long long)(1024 >> 4) << 32 |
-           1ull << 46 | 2ull << 61;
-}
 // fp32 accumulators, half-precision operands, M = 128; mn: the second operand is MN-major.
 __host__ __device__ constexpr uint32_t tc_idesc(int n, bool mn) { return 1u << 4 | (mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }
 
@@ -126,34 +126,35 @@ template <int D> struct TileLayout {
 };
 static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
 
-// Bits of the slots that token i of a run's sequence sees among the step's tokens [j0, j0 + 32) (negative j: the prefix).
-__device__ __forceinline__ uint32_t kv_sees32(const KvStep& st, int b, int i, int tokens, int j0) {
+// Bits of the slots that token i of a run's sequence sees among the step's tokens [j0, j0 + 64) (negative j: the prefix).
+__device__ __forceinline__ uint64_t kv_sees64(const KvStep& st, int b, int i, int tokens, int j0) {
     const int end = tokens - j0;                             // bits at or beyond are behind the last slot
-    const uint32_t inside = end >= 32 ? 0xFFFFFFFFu : (end <= 0 ? 0u : (1u << end) - 1u);
+    const uint64_t inside = end >= 64 ? ~0ull : (end <= 0 ? 0ull : (1ull << end) - 1ull);
     if (!st.mask) {
         const int n = i + 1 - j0;
-        return inside & (n >= 32 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << n) - 1u));
+        return inside & (n >= 64 ? ~0ull : (n <= 0 ? 0ull : (1ull << n) - 1ull));
     }
-    uint32_t v = 0;
-    if (j0 <= 0) v = j0 <= -32 ? 0xFFFFFFFFu : (2u << -j0) - 1u;                   // the prefix and the root (j <= 0)
-    if (i > 0 && j0 > -32) {
+    uint64_t v = 0;
+    if (j0 <= 0) v = j0 <= -64 ? ~0ull : (2ull << -j0) - 1ull;                     // the prefix and the root (j <= 0)
+    if (i > 0 && j0 > -64) {
         const int W = (st.T - 1 + 63) >> 6, at = j0 - 1;
         const uint64_t* m = st.mask + ((long long)b * (st.T - 1) + i - 1) * W;
-        if (at < 0) v |= -at < 32 ? (uint32_t)(m[0] << -at) : 0u;
+        if (at < 0) v |= -at < 64 ? m[0] << -at : 0ull;
         else {
             const int w = at >> 6, s = at & 63;
-            if (w < W) v |= (uint32_t)(m[w] >> s);
-            if (s > 32 && w + 1 < W) v |= (uint32_t)(m[w + 1] << (64 - s));
+            if (w < W) v |= m[w] >> s;
+            if (s > 0 && w + 1 < W) v |= m[w + 1] << (64 - s);
         }
     }
-    if (i >= j0 && i < j0 + 32) v |= 1u << (i - j0);
+    if (i >= j0 && i < j0 + 64) v |= 1ull << (i - j0);
     return v & inside;
 }
 
-// A row's sums are kept relative to a reference 2^10 below the largest score at the time; the largest may grow by another 2^5 before they
-// are brought to a new reference.  So probabilities of up to 2^15 use the range of half precision (rounded by 2^-11 of each down to 2^-24
-// of the largest; relative to the largest alone, small ones would lose bits that matter where the large ones' values cancel).
-constexpr float kLift = 10.f, kGrowth = 5.f;
+// A row's sums are kept relative to a reference 2^5 below the largest score at the time; the largest may grow by another 2^10 before they
+// are brought to a new reference.  So probabilities of up to 2^15 use the range of half precision (rounded by 2^-11 of each down to 2^-19
+// of the largest, by 2^-30 of the largest below; relative to the largest alone, small ones would lose bits that matter where the large
+// ones' values cancel).
+constexpr float kLift = 5.f, kGrowth = 10.f;
 
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {         // NaN if any is
     float d;
@@ -268,11 +269,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 for (int half = 0; half < 2; ++half) {
                     const int j0 = kt * kTileKeys + half * 64 - r.len;             // the first slot, as a token of the step
                     const bool edge = j0 + 64 > 0;
-                    uint32_t see[2] = {0, 0};
-                    if (edge && busy) {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) see[c] = kv_sees32(a.step, r.b, token, r.tokens, j0 + c * 32);
-                    }
+                    const uint64_t see = edge && busy ? kv_sees64(a.step, r.b, token, r.tokens, j0) : 0ull;
                     wait(L::kBarS + 2 * X + half, tiles & 1);
                     tc_fence_after();
                     if (busy) {
@@ -289,7 +286,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
 #pragma unroll
                             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) x[c][i] = see[c] >> i & 1 ? x[c][i] : -INFINITY;
+                                for (int i = 0; i < 32; ++i) x[c][i] = (uint32_t)(see >> c * 32) >> i & 1 ? x[c][i] : -INFINITY;
                         }
                         float top4[4];
 #pragma unroll
@@ -569,92 +566,84 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
     } else if (warp == 12) {
         // ---- products: one lane issues ----
-        constexpr uint32_t kScores = tc_idesc(64, false), kOutputs = tc_idesc(D, true);
-        const uint32_t sq = smem_u32(smem + L::kQ), sk = smem_u32(smem + L::kK), sv = smem_u32(smem + L::kV);
-        uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
-        auto scores = [&](int X, int Q, uint32_t stage, int half) {
-            if (elect_one()) {
+        if (elect_one()) {
+            constexpr uint32_t kScores = tc_idesc(64, false), kOutputs = tc_idesc(D, true), kHalf = 64 * 128 >> 4, kStageStep = L::kOperand >> 4;
+            const uint32_t dq = tc_desc(smem_u32(smem + L::kQ), 16), dk = tc_desc(smem_u32(smem + L::kK), 16), dv = tc_desc(smem_u32(smem + L::kV), 128 * 128);
+            auto wait1 = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_thread(bars + bar, parity, a.status); };
+            uint32_t done = 0, nrun = 0, tiles[2] = {0, 0};
+            auto scores = [&](int X, int Q, uint32_t stage, int half) {
+                const uint32_t d = tmem + L::kColS + X * 128 + half * 64, q = dq + Q * kStageStep, k0 = dk + stage * kStageStep + half * kHalf;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t at = (k >> 2) * (128 * 128) + (k & 3) * 32;
-                    tc_mma_ss(tmem + L::kColS + X * 128 + half * 64, tc_desc(sq + Q * L::kOperand + at, 16),
-                              tc_desc(sk + stage * L::kOperand + half * (64 * 128) + at, 16), kScores, k > 0);
+                    const uint32_t at = ((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4;
+                    tc_mma_ss(d, q + at, k0 + at, kScores, k > 0);
                 }
                 tc_commit(bars + L::kBarS + 2 * X + half);
-            }
-            __syncwarp();
-        };
-        auto outputs = [&](int X, uint32_t stage, int half, bool add) {
-            wait(L::kBarP + 2 * X + half, tiles[X] & 1);
-            tiles[X] += half;
-            tc_fence_after();
-            if (elect_one()) {
+            };
+            auto outputs = [&](int X, uint32_t stage, int half, bool add) {
+                wait1(L::kBarP + 2 * X + half, tiles[X] & 1);
+                tiles[X] += half;
+                tc_fence_after();
+                const uint32_t d = tmem + L::kColO + X * D, p = tmem + L::kColS + X * 128 + half * 64, v = dv + stage * kStageStep + half * kHalf;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    tc_mma_ts(tmem + L::kColO + X * D, tmem + L::kColS + X * 128 + half * 64 + k * 8,
-                              tc_desc(sv + stage * L::kOperand + half * (64 * 128) + k * 2048, 128 * 128), kOutputs, add || k > 0);
+                for (int k = 0; k < 4; ++k) tc_mma_ts(d, p + k * 8, v + k * (2048 >> 4), kOutputs, add || k > 0);
                 tc_commit(bars + L::kBarO + 2 * X + half);
-            }
-            __syncwarp();
-        };
-        auto keys = [&](uint32_t tile) {                     // waits for a tile's keys
-            wait(L::kBarKFull + (tile & 1), tile >> 1 & 1);
-            tc_fence_after();
-        };
-        auto commit = [&](int bar) {
-            if (elect_one()) tc_commit(bars + bar);
-            __syncwarp();
-        };
-        while (walk.next(a, r)) {
-            const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
-            const int n = r.k1 - r.k0;
-            wait(L::kBarQ, nrun & 1);
-            ++nrun;
-            if (single) {                                    // one row tile: the two groups take its key tiles in turn
-                for (int i = 0; i < min(n, 2); ++i) {
-                    keys(done + i);
-                    for (int half = 0; half < 2; ++half) scores(i, 0, (done + i) & 1, half);
-                    commit(L::kBarKFree + ((done + i) & 1));
-                }
-                for (int i = 0; i < n; ++i, ++done) {
-                    const uint32_t stage = done & 1;
-                    wait(L::kBarVFull + stage, done >> 1 & 1);
-                    for (int half = 0; half < 2; ++half) {
-                        outputs(i & 1, stage, half, i > 1 || half);
-                        if (i + 2 < n) {
-                            if (half == 0) keys(done + 2);
-                            scores(i & 1, 0, stage, half);
-                        }
+            };
+            auto keys = [&](uint32_t tile) {                 // waits for a tile's keys
+                wait1(L::kBarKFull + (tile & 1), tile >> 1 & 1);
+                tc_fence_after();
+            };
+            while (walk.next(a, r)) {
+                const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
+                const int n = r.k1 - r.k0;
+                wait1(L::kBarQ, nrun & 1);
+                ++nrun;
+                if (single) {                                // one row tile: the two groups take its key tiles in turn
+                    for (int i = 0; i < min(n, 2); ++i) {
+                        keys(done + i);
+                        for (int half = 0; half < 2; ++half) scores(i, 0, (done + i) & 1, half);
+                        tc_commit(bars + L::kBarKFree + ((done + i) & 1));
                     }
-                    commit(L::kBarVFree + stage);
-                    if (i + 2 < n) commit(L::kBarKFree + stage);
-                }
-            } else {                                         // two row tiles in turn
-                keys(done);
-                for (int half = 0; half < 2; ++half)
-                    for (int X = 0; X < 2; ++X) scores(X, X, done & 1, half);
-                commit(L::kBarKFree + (done & 1));
-                for (int i = 0; i < n; ++i, ++done) {
-                    const uint32_t stage = done & 1, next = (done + 1) & 1;
-                    const bool more = i + 1 < n;
-                    wait(L::kBarVFull + stage, done >> 1 & 1);
-                    for (int half = 0; half < 2; ++half)
-                        for (int X = 0; X < 2; ++X) {
-                            outputs(X, stage, half, i > 0 || half);
-                            if (more) {
-                                if (X == 0 && half == 0) keys(done + 1);
-                                scores(X, X, next, half);
+                    for (int i = 0; i < n; ++i, ++done) {
+                        const uint32_t stage = done & 1;
+                        wait1(L::kBarVFull + stage, done >> 1 & 1);
+                        for (int half = 0; half < 2; ++half) {
+                            outputs(i & 1, stage, half, i > 1 || half);
+                            if (i + 2 < n) {
+                                if (half == 0) keys(done + 2);
+                                scores(i & 1, 0, stage, half);
                             }
                         }
-                    commit(L::kBarVFree + stage);
-                    if (more) commit(L::kBarKFree + next);
+                        tc_commit(bars + L::kBarVFree + stage);
+                        if (i + 2 < n) tc_commit(bars + L::kBarKFree + stage);
+                    }
+                } else {                                     // two row tiles in turn
+                    keys(done);
+                    for (int half = 0; half < 2; ++half)
+                        for (int X = 0; X < 2; ++X) scores(X, X, done & 1, half);
+                    tc_commit(bars + L::kBarKFree + (done & 1));
+                    for (int i = 0; i < n; ++i, ++done) {
+                        const uint32_t stage = done & 1, next = (done + 1) & 1;
+                        const bool more = i + 1 < n;
+                        wait1(L::kBarVFull + stage, done >> 1 & 1);
+                        for (int half = 0; half < 2; ++half)
+                            for (int X = 0; X < 2; ++X) {
+                                outputs(X, stage, half, i > 0 || half);
+                                if (more) {
+                                    if (X == 0 && half == 0) keys(done + 1);
+                                    scores(X, X, next, half);
+                                }
+                            }
+                        tc_commit(bars + L::kBarVFree + stage);
+                        if (more) tc_commit(bars + L::kBarKFree + next);
+                    }
                 }
             }
+            // everything issued is complete before TMEM is given back, also after a wait that ran out
+            tc_commit(bars + L::kBarEnd);
+            mbar_wait_thread(bars + L::kBarEnd, 0, a.status);
         }
-        // everything issued is complete before TMEM is given back, also after a wait that ran out
-        if (elect_one()) tc_commit(bars + L::kBarEnd);
         __syncwarp();
-        mbar_wait_warp(bars + L::kBarEnd, 0, a.status);
     }
     tc_fence_before();
     __syncthreads();
