@@ -105,8 +105,8 @@ def lib():
         L.opt_tree_kv_workspace_bytes.argtypes = [C.POINTER(KVConfig)]
         L.opt_tree_kv_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(KVConfig)]
         L.opt_tree_kv_destroy.argtypes = [C.c_void_p]
-        rows, cache, step = C.POINTER(KVRows), C.POINTER(KVCacheC), C.POINTER(KVStepC)
-        L.opt_tree_kv_append.argtypes = [C.c_void_p, cache, C.c_int32, rows, rows, rows, rows, step, C.POINTER(KVTurn), C.c_void_p]
+        rows, cache, step = C.c_void_p, C.c_void_p, C.c_void_p        # (plain addresses are handed over faster than typed pointers)
+        L.opt_tree_kv_append.argtypes = [C.c_void_p, cache, C.c_int32, rows, rows, rows, rows, step, C.c_void_p, C.c_void_p]
         L.opt_tree_kv_attend.argtypes = [C.c_void_p, cache, C.c_int32, rows, step, C.c_float, rows, C.c_void_p, C.c_void_p]
         L.opt_tree_kv_compact.argtypes = [C.c_void_p, cache, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         L.opt_tree_kv_last_device_status.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
@@ -336,34 +336,49 @@ def verify_static(cfg: Config, tree: Tree, target: torch.Tensor, root_token: tor
 
 # ---- the paged 8-bit cache of the target model's attention layers ----
 
+_current_device, _current_stream = torch.cuda.current_device, lambda index: torch.cuda.current_stream(index).cuda_stream
+if torch.cuda.is_available():            # the same without the wrappers' checks, which cost more than the library's launch
+    _current_device = getattr(torch._C, "_cuda_getDevice", _current_device)
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+
 _ROW_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+_F8, _F32, _I32, _I64 = torch.float8_e4m3fn, torch.float32, torch.int32, torch.int64
 
 
-def _plain(t, name: str, dtype, shape, device):
-    """A contiguous tensor of this type, shape and device (or None)."""
-    if t is not None and (t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous()):
-        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr() if t is not None else None
+def _index(device: torch.device) -> int:
+    """A device as Tensor.get_device() numbers it."""
+    return device.index if device.type == "cuda" else -1
+
+
+def _addr(t, name: str, dtype, shape, index: int):
+    """Address of a contiguous tensor of this type, shape and device; None for None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on device {index} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class KVCache:
     """Cache tensors (torch owns the memory): k, v [layers][num_pages][kv_heads][page][head_dim] float8_e4m3fn, k_scale, v_scale
-    [layers][num_pages][kv_heads] float32, block_table [B][max_pages] int32 (see opt_tree_kv_cache)."""
+    [layers][num_pages][kv_heads] float32, block_table [B][max_pages] int32 (see opt_tree_kv_cache).  One object serves any number of calls."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "block_table", "c")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "block_table", "shape", "table_shape", "index", "c", "c_addr")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor):
-        f8, dev = torch.float8_e4m3fn, k.device
-        if k.dim() != 5 or block_table.dim() != 2:
+        shape, table, index = k.shape, block_table.shape, k.get_device()
+        if len(shape) != 5 or len(table) != 2:
             raise ValueError("k: [layers][num_pages][kv_heads][page][head_dim], block_table: [B][max_pages]")
-        self.c = KVCacheC(_plain(k, "k", f8, k.shape, dev), _plain(v, "v", f8, k.shape, dev),
-                          _plain(k_scale, "k_scale", torch.float32, k.shape[:3], dev), _plain(v_scale, "v_scale", torch.float32, k.shape[:3], dev),
-                          _plain(block_table, "block_table", torch.int32, block_table.shape, dev))
+        scales = shape[:3]
+        self.c = KVCacheC(_addr(k, "k", _F8, shape, index), _addr(v, "v", _F8, shape, index), _addr(k_scale, "k_scale", _F32, scales, index),
+                          _addr(v_scale, "v_scale", _F32, scales, index), _addr(block_table, "block_table", _I32, table, index))
+        self.c_addr = C.addressof(self.c)
         self.k, self.v, self.k_scale, self.v_scale, self.block_table = k, v, k_scale, v_scale, block_table
+        self.shape, self.table_shape, self.index = shape, table, index
 
 
 class KVStep:
-    """A step's tokens (see opt_tree_kv_step): the root and `nodes` nodes of each sequence."""
+    """A step's tokens (see opt_tree_kv_step): the root and `nodes` nodes of each sequence.  One object serves a step's calls for all layers."""
 
     __slots__ = ("kv_len", "nodes", "base_pos", "position_ids", "mask")
 
@@ -371,11 +386,14 @@ class KVStep:
                  position_ids: torch.Tensor | None = None, mask: torch.Tensor | None = None):
         self.kv_len, self.nodes, self.base_pos, self.position_ids, self.mask = kv_len, nodes, base_pos, position_ids, mask
 
-    def c_struct(self, B: int, T: int, device) -> KVStepC:
-        i32, one = torch.int32, (B,)
-        return KVStepC(B, T, _plain(self.kv_len, "kv_len", i32, one, device), _plain(self.nodes, "nodes", i32, one, device),
-                       _plain(self.base_pos, "base_pos", i32, one, device), _plain(self.position_ids, "position_ids", i32, (B, T - 1), device),
-                       _plain(self.mask, "mask", torch.int64, (B, T - 1, (T + 62) // 64), device) if T > 1 else None)
+    def c_struct(self, B: int, T: int, device: torch.device) -> KVStepC:
+        return self._struct(B, T, _index(device))
+
+    def _struct(self, B: int, T: int, index: int) -> KVStepC:
+        one = (B,)
+        return KVStepC(B, T, _addr(self.kv_len, "kv_len", _I32, one, index), _addr(self.nodes, "nodes", _I32, one, index),
+                       _addr(self.base_pos, "base_pos", _I32, one, index), _addr(self.position_ids, "position_ids", _I32, (B, T - 1), index),
+                       _addr(self.mask, "mask", _I64, (B, T - 1, (T + 62) // 64), index) if T > 1 else None)
 
 
 class TreeKV:
@@ -388,17 +406,22 @@ class TreeKV:
             raise RuntimeError("no CUDA device: the OPT-Tree library has no CPU fallback")
         if dtype not in _ROW_TYPES:
             raise ValueError(f"dtype: bfloat16 or float16, not {dtype}")
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        self.device = torch.device("cuda" if device is None else device)
         if self.device.type != "cuda":
             raise ValueError(f"device: a CUDA device, not {self.device}")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = dtype
         self.cfg = KVConfig(q_heads, kv_heads, head_dim, page, num_pages, max_pages, max_batch, max_step, layers, _ROW_TYPES[dtype])
-        self._cache_shape = (layers, num_pages, kv_heads, page, head_dim)
-        self._scale = head_dim ** -0.5
+        self._sizes()
         with torch.cuda.device(self.device):
             _check(lib().opt_tree_kv_create(C.byref(self._kv), C.byref(self.cfg)), "opt_tree_kv_create")
+
+    def _sizes(self):
+        c = self.cfg
+        self._cache_shape = (c.layers, c.num_pages, c.kv_heads, c.page, c.head_dim)
+        self._q_heads, self._kv_heads, self._D, self._max_pages = c.q_heads, c.kv_heads, c.head_dim, c.max_pages
+        self._scale, self._at = c.head_dim ** -0.5, _index(self.device)
 
     def close(self):
         if self._kv:
@@ -413,70 +436,79 @@ class TreeKV:
 
     def alloc_cache(self, block_table: torch.Tensor) -> KVCache:
         L, N, H, P, D = self._cache_shape
-        k, v = (torch.zeros((L, N, H, P, D), dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn) for _ in range(2))
-        ks, vs = (torch.ones((L, N, H), dtype=torch.float32, device=self.device) for _ in range(2))
+        k, v = (torch.zeros((L, N, H, P, D), dtype=torch.uint8, device=self.device).view(_F8) for _ in range(2))
+        ks, vs = (torch.ones((L, N, H), dtype=_F32, device=self.device) for _ in range(2))
         return KVCache(k, v, ks, vs, block_table)
 
     def _rows(self, t: torch.Tensor, name: str, B: int, T: int, heads: int) -> KVRows:
-        if t.dtype != self.dtype or t.shape != (B, T, heads, self.cfg.head_dim) or t.device != self.device or t.stride(3) != 1:
-            raise ValueError(f"{name}: {self.dtype} [{B}][{T}][{heads}][{self.cfg.head_dim}] with contiguous rows on {self.device} is needed, "
-                             f"not {t.dtype} {tuple(t.shape)} on {t.device}")
-        return KVRows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+        st = t.stride()
+        if t.dtype is self.dtype and t.shape == (B, T, heads, self._D) and t.get_device() == self._at and st[3] == 1:
+            return KVRows(t.data_ptr(), st[0], st[1], st[2])
+        raise ValueError(f"{name}: {self.dtype} [{B}][{T}][{heads}][{self._D}] with contiguous rows on {self.device} is needed, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
 
-    def _check_cache(self, cache: KVCache, B: int):
-        if cache.k.shape != self._cache_shape or cache.k.device != self.device or cache.block_table.shape[1] != self.cfg.max_pages or cache.block_table.shape[0] < B:
-            raise ValueError(f"cache: pages {self._cache_shape} and a block table [{B}][{self.cfg.max_pages}] on {self.device} are needed, "
-                             f"not {tuple(cache.k.shape)} and {tuple(cache.block_table.shape)} on {cache.k.device}")
+    def _cache(self, cache: KVCache, B: int) -> int:
+        table = cache.table_shape
+        if cache.shape == self._cache_shape and cache.index == self._at and table[1] == self._max_pages and table[0] >= B:
+            return cache.c_addr
+        raise ValueError(f"cache: pages {self._cache_shape} and a block table [{B}][{self._max_pages}] on {self.device} are needed, "
+                         f"not {tuple(cache.shape)} and {tuple(table)} on {cache.k.device}")
 
-    def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+    def _call(self, name: str, *args):
+        """Calls with the handle's device current and its current stream as the last argument."""
+        f = getattr(lib(), name)
+        if _current_device() == self._at:
+            code = f(self._kv, *args, _current_stream(self._at))
+        else:
+            with torch.cuda.device(self.device):
+                code = f(self._kv, *args, _current_stream(self._at))
+        if code != OK:
+            raise OptTreeError(code, name)
 
     def append(self, cache: KVCache, layer: int, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, step: KVStep,
                cos_sin: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
                interleaved: bool = False, q_out: torch.Tensor | None = None) -> torch.Tensor | None:
         """opt_tree_kv_append: norm and rotation of q and k, k and v into the cache; returns the rotated queries (q_out; None if q is None)."""
-        c, (B, T) = self.cfg, k.shape[:2]
-        self._check_cache(cache, B)
-        if q is not None and q_out is None:
-            q_out = torch.empty((B, T, c.q_heads, c.head_dim), dtype=self.dtype, device=self.device)
-        qr, qo = (C.byref(self._rows(t, n, B, T, c.q_heads)) if q is not None else None for t, n in ((q, "q"), (q_out, "q_out")))
-        turn = KVTurn(None, 0, 0, int(interleaved), _plain(q_norm, "q_norm", self.dtype, (c.head_dim,), self.device),
-                      _plain(k_norm, "k_norm", self.dtype, (c.head_dim,), self.device), eps)
+        B, T = k.shape[:2]
+        at, rows, heads = self._at, self._rows, self._kv_heads
+        qr = qo = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty((B, T, self._q_heads, self._D), dtype=self.dtype, device=self.device)
+            qr, qo = C.byref(rows(q, "q", B, T, self._q_heads)), C.byref(rows(q_out, "q_out", B, T, self._q_heads))
+        turn = KVTurn(None, 0, 0, bool(interleaved), None, None, eps)
+        if q_norm is not None:
+            turn.q_norm = _addr(q_norm, "q_norm", self.dtype, (self._D,), at)
+        if k_norm is not None:
+            turn.k_norm = _addr(k_norm, "k_norm", self.dtype, (self._D,), at)
         if cos_sin is not None:
-            turn.cos_sin = _plain(cos_sin, "cos_sin", torch.float32, cos_sin.shape, self.device)
-            turn.positions, turn.rot_dim = cos_sin.shape
-        with torch.cuda.device(self.device):
-            _check(lib().opt_tree_kv_append(self._kv, C.byref(cache.c), layer, qr, C.byref(self._rows(k, "k", B, T, c.kv_heads)),
-                                            C.byref(self._rows(v, "v", B, T, c.kv_heads)), qo, C.byref(step.c_struct(B, T, self.device)),
-                                            C.byref(turn), self._stream()), "opt_tree_kv_append")
+            turn.positions, turn.rot_dim = shape = cos_sin.shape
+            turn.cos_sin = _addr(cos_sin, "cos_sin", _F32, shape, at)
+        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, C.byref(rows(k, "k", B, T, heads)), C.byref(rows(v, "v", B, T, heads)), qo,
+                   C.byref(step._struct(B, T, at)), C.byref(turn))
         return q_out
 
     def attend(self, cache: KVCache, layer: int, q: torch.Tensor, step: KVStep, scale: float | None = None, out: torch.Tensor | None = None,
                lse: torch.Tensor | None = None) -> torch.Tensor:
         """opt_tree_kv_attend: attention of the step's tokens over the cache; scale defaults to head_dim ** -0.5."""
-        c, (B, T) = self.cfg, q.shape[:2]
-        self._check_cache(cache, B)
+        B, T = q.shape[:2]
+        heads = self._q_heads
         if out is None:
-            out = torch.empty((B, T, c.q_heads, c.head_dim), dtype=self.dtype, device=self.device)
-        with torch.cuda.device(self.device):
-            _check(lib().opt_tree_kv_attend(self._kv, C.byref(cache.c), layer, C.byref(self._rows(q, "q", B, T, c.q_heads)),
-                                            C.byref(step.c_struct(B, T, self.device)), self._scale if scale is None else scale,
-                                            C.byref(self._rows(out, "out", B, T, c.q_heads)),
-                                            _plain(lse, "lse", torch.float32, (B, T, c.q_heads), self.device), self._stream()), "opt_tree_kv_attend")
+            out = torch.empty((B, T, heads, self._D), dtype=self.dtype, device=self.device)
+        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, C.byref(self._rows(q, "q", B, T, heads)), C.byref(step._struct(B, T, self._at)),
+                   self._scale if scale is None else scale, C.byref(self._rows(out, "out", B, T, heads)),
+                   _addr(lse, "lse", _F32, (B, T, heads), self._at))
         return out
 
     def compact(self, cache: KVCache, kv_len: torch.Tensor, kv_gather: torch.Tensor, kv_keep: torch.Tensor,
                 new_len: torch.Tensor | None = None) -> torch.Tensor:
         """opt_tree_kv_compact: the accepted path's entries of all layers to the end of the prefix; returns the new lengths."""
-        B, G = kv_gather.shape
-        self._check_cache(cache, B)
+        B, G = shape = kv_gather.shape
         if new_len is None:
-            new_len = torch.empty(B, dtype=torch.int32, device=self.device)
-        i32, dev = torch.int32, self.device
-        with torch.cuda.device(self.device):
-            _check(lib().opt_tree_kv_compact(self._kv, C.byref(cache.c), _plain(kv_len, "kv_len", i32, (B,), dev),
-                                             _plain(kv_gather, "kv_gather", i32, (B, G), dev), _plain(kv_keep, "kv_keep", i32, (B,), dev), G, B,
-                                             _plain(new_len, "new_len", i32, (B,), dev), self._stream()), "opt_tree_kv_compact")
+            new_len = torch.empty_like(kv_len)
+        one, at = (B,), self._at
+        self._call("opt_tree_kv_compact", self._cache(cache, B), _addr(kv_len, "kv_len", _I32, one, at), _addr(kv_gather, "kv_gather", _I32, shape, at),
+                   _addr(kv_keep, "kv_keep", _I32, one, at), G, B, _addr(new_len, "new_len", _I32, one, at))
         return new_len
 
     def device_status(self) -> int:
