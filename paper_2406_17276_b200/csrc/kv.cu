@@ -15,6 +15,7 @@ struct opt_tree_kv {
     void* base;                          // status word, arrival counters, parts
     int* status;
     int* arrived;
+    ot::KvRun* cuts;
     float* parts;
     int device, sms;
     int64_t launches;
@@ -71,15 +72,16 @@ template <int D, class T> AppendKernel append_variant(int page, int* threads) {
 }
 
 using AttendKernel = void (*)(ot::KvAttend);
-using JoinKernel = void (*)(ot::KvAttend, int);
-struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads; JoinKernel join; };
+using JoinKernel = void (*)(ot::KvAttend);
+struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads, rows, keys; JoinKernel join; };
 template <int D, int NT, class T> AttendVariant few_variant() {
-    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads, nullptr};
+    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads, 8 * NT, ot::kFewKeys, nullptr};
 }
 template <int D, class T> AttendVariant attend_variant(int rows) {
     if (rows <= 8) return few_variant<D, 1, T>();
     if (rows <= 16) return few_variant<D, 2, T>();
-    return AttendVariant{ot::kv_attend_tiles_kernel<D, T>, (size_t)ot::TileLayout<D>::kBytes, 1, ot::kTileThreads, ot::kv_join_kernel<D, T>};
+    return AttendVariant{ot::kv_attend_tiles_kernel<D, T>, (size_t)ot::TileLayout<D>::kBytes, 1, ot::kTileThreads, 2 * ot::kTileRows, ot::kTileKeys,
+                         ot::kv_join_kernel<D, T>};
 }
 // The kernel for `rows` query rows per sequence and key head at most.
 AttendVariant attend_for(const opt_tree_kv_config& c, int rows) {
@@ -112,7 +114,7 @@ size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config* cfg) {
         cudaGetLastError();
         sms = 148;                                   // no device here: the size on a B200
     }
-    return 256 + align256(sms * kMaxParts * sizeof(int)) + sms * parts_per_sm(*cfg);
+    return 256 + align256(sms * kMaxParts * sizeof(int)) + align256(sms * sizeof(ot::KvRun)) + sms * parts_per_sm(*cfg);
 }
 
 int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
@@ -141,7 +143,8 @@ int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
     }
     for (int rows : kVariantRows) {
         const AttendVariant v = attend_for(*cfg, rows);
-        if (cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem) != cudaSuccess) {
+        cudaFuncAttributes got;
+        if (cudaFuncGetAttributes(&got, v.kernel) != cudaSuccess || (v.join && got.numRegs != ot::kRegsLaunch) || cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem) != cudaSuccess) {
             cudaGetLastError();
             cudaFree(kv->base);
             delete kv;
@@ -151,7 +154,9 @@ int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
     char* at = static_cast<char*>(kv->base);
     kv->status = reinterpret_cast<int*>(at);
     kv->arrived = reinterpret_cast<int*>(at + 256);
-    kv->parts = reinterpret_cast<float*>(at + 256 + align256(kv->sms * kMaxParts * sizeof(int)));
+    at += 256 + align256(kv->sms * kMaxParts * sizeof(int));
+    kv->cuts = reinterpret_cast<ot::KvRun*>(at);
+    kv->parts = reinterpret_cast<float*>(at + align256(kv->sms * sizeof(ot::KvRun)));
     *out = kv;
     return OPT_TREE_OK;
 }
@@ -232,12 +237,14 @@ int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
     a.by_group = ot::FixedDiv::by((unsigned)a.group);
     a.parts = kv->parts;
     a.arrived = kv->arrived;
+    a.cuts = kv->cuts;
     a.status = kv->status;
     const AttendVariant v = attend_for(kv->cfg, step->T * a.group);
+    if (ot::kv_cost_bound(kv->shape, step->B, step->T, v.rows, v.keys) > 0x7FFFFFFFll) return OPT_TREE_ERR_UNSUPPORTED;
     const int grid = kv->sms * v.per_sm;
     launch_after(v.kernel, dim3(grid), dim3(v.threads), v.smem, static_cast<cudaStream_t>(stream), a);
     if (v.join) {
-        launch_after(v.join, dim3(grid, ot::kJoinBlocks), dim3(256), 0, static_cast<cudaStream_t>(stream), a, grid);
+        launch_after(v.join, dim3(grid, ot::kJoinBlocks), dim3(256), 0, static_cast<cudaStream_t>(stream), a);
         kv->launches++;
     }
     kv->launches++;

@@ -27,6 +27,7 @@ struct KvAttend {
     int wide_q, wide_out;
     float* parts;                        // [2 * grid][part_floats]
     int* arrived;                        // [grid], zero between calls
+    struct KvRun* cuts;                  // [grid]: the cut row tile that began in each CTA, or b < 0
     int* status;
 };
 
@@ -50,14 +51,23 @@ struct KvRun {
     int first, last;                     // CTAs that hold the row tile's first and last tile: more than one if it is cut
 };
 
-// Walks the run of tiles of one CTA of a grid.  kRows rows and kKeys keys a tile.  Every warp keeps its own copy (no shared memory, no
-// barrier); the lengths come from the cache after the first warp.
-template <int kRows, int kKeys>
+// Walks the run of tiles of one CTA of a grid.  kRows rows and kKeys keys a tile.  kHalves: a row tile of at most kRows / 2 rows costs half
+// of the others.  A run is an equal share of the cost; a key tile belongs to the CTA in whose share it begins (shares are no smaller than a
+// tile, so none is empty).  Every warp keeps its own copy (no shared memory, no barrier); the lengths come from the cache after the
+// first warp.
+template <int kRows, int kKeys, bool kHalves>
 struct KvWalk {
-    long long total, pos, end, base;     // tiles; base: first tile of sequence b
+    static constexpr int kMost = kHalves ? 2 : 1;            // cost of a key tile of a full row tile
+    static constexpr int kAhead = 4;                         // groups of 32 sequences whose lengths are loaded together
+    // Cost of everything, share of each CTA (and what is left over), next, end of the share; base: where sequence b begins.  The host has
+    // seen to it that costs fit (see kv_cost_bound); with 32 bits there are no long divisions.
+    unsigned total, share, left, pos, end, base;
     int cta, grid, b;
 
     __device__ __forceinline__ static int row_tiles(const KvAttend& a, int tokens) { return (tokens * a.group + kRows - 1) / kRows; }
+    __device__ __forceinline__ static int cost_of(const KvAttend& a, int tokens, int rt) {
+        return kHalves && tokens * a.group - rt * kRows > kRows / 2 ? 2 : 1;
+    }
     // In a chain a row tile sees no further than its last token.
     __device__ __forceinline__ static int keys_of(const KvAttend& a, int len, int tokens, int rt) {
         if (a.step.mask) return len + tokens;
@@ -65,106 +75,145 @@ struct KvWalk {
         return len + min(tokens, last + 1);
     }
     __device__ __forceinline__ static int tiles_of(const KvAttend& a, int len, int tokens, int rt) { return (keys_of(a, len, tokens, rt) + kKeys - 1) / kKeys; }
-    // Tiles of one key head of a sequence.
-    __device__ __forceinline__ static long long head_tiles(const KvAttend& a, int len, int tokens) {
+    // Cost of one key head of a sequence.
+    __device__ __forceinline__ static unsigned head_cost(const KvAttend& a, int len, int tokens) {
         const int n = row_tiles(a, tokens);
         if (n == 0) return 0;
-        if (a.step.mask) return (long long)n * tiles_of(a, len, tokens, 0);
-        long long s = 0;
-        for (int rt = 0; rt < n; ++rt) s += tiles_of(a, len, tokens, rt);
+        if (a.step.mask || n == 1) return (unsigned)tiles_of(a, len, tokens, 0) * (kMost * (n - 1) + cost_of(a, tokens, n - 1));
+        unsigned s = 0;
+#pragma unroll 1
+        for (int rt = 0; rt < n; ++rt) s += tiles_of(a, len, tokens, rt) * cost_of(a, tokens, rt);
         return s;
     }
-    __device__ __forceinline__ static long long sequence_tiles(const KvAttend& a, int b) {
+    __device__ __forceinline__ static unsigned sequence_cost(const KvAttend& a, int b) {
         int len, tokens;
         if (b >= a.step.B || !kv_sequence(a.shape, a.step, b, len, tokens, a.status)) return 0;
-        return head_tiles(a, len, tokens) * a.shape.kv_heads;
+        return head_cost(a, len, tokens) * a.shape.kv_heads;
     }
-    __device__ __forceinline__ static long long warp_scan(long long v) {
+    __device__ __forceinline__ static unsigned warp_scan(unsigned v) {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long u = __shfl_up_sync(0xFFFFFFFFu, v, o);
+            const unsigned u = __shfl_up_sync(0xFFFFFFFFu, v, o);
             if (lane >= o) v += u;
         }
         return v;
     }
+    __device__ __forceinline__ unsigned begins(int c) const { return share * c + left * c / grid; }       // total * c / grid
     // false: nothing for this CTA.
-    __device__ bool begin(const KvAttend& a, int which, int ctas) {
-        const int lane = threadIdx.x & 31;
+    __device__ __forceinline__ bool begin(const KvAttend& a, int which, int ctas) {
+        unsigned incl[kAhead];
         total = 0;
-        long long incl = 0;
-        for (int b0 = 0; b0 < a.step.B; b0 += 32) {
-            incl = warp_scan(sequence_tiles(a, b0 + lane));
-            total += __shfl_sync(0xFFFFFFFFu, incl, 31);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) incl[k] = k * 32 < a.step.B ? sequence_cost(a, k * 32 + (threadIdx.x & 31)) : 0u;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (k * 32 >= a.step.B) break;
+            incl[k] = warp_scan(incl[k]);
+            total += __shfl_sync(0xFFFFFFFFu, incl[k], 31);
         }
+#pragma unroll 1
+        for (int b0 = kAhead * 32; b0 < a.step.B; b0 += 32) total += __shfl_sync(0xFFFFFFFFu, warp_scan(sequence_cost(a, b0 + (threadIdx.x & 31))), 31);
         cta = which;
-        grid = (int)min((long long)ctas, total);
+        grid = min(ctas, (int)((total + kMost - 1) / kMost));
         if (cta >= grid) return false;
-        pos = total * cta / grid;
-        end = total * (cta + 1) / grid;
-        find(a, incl);
-        return true;
-    }
-    // Sets b and base to the sequence that holds tile pos; incl: this lane's inclusive count where all sequences fit in a warp.
-    __device__ void find(const KvAttend& a, long long incl) {
-        const int lane = threadIdx.x & 31;
+        share = total / grid;
+        if (kMost > 1 && grid > 1 && share < kMost) share = total / --grid;
+        if (cta >= grid) return false;
+        left = total - share * grid;
+        pos = begins(cta);
+        end = begins(cta + 1);
+        // the sequence that holds pos
         base = 0;
         b = 0;
-        for (int b0 = 0; b0 < a.step.B; b0 += 32) {
-            if (a.step.B > 32) incl = warp_scan(sequence_tiles(a, b0 + lane));
-            const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > pos);
-            if (over) {
-                const int l = __ffs(over) - 1;
-                const long long before = __shfl_sync(0xFFFFFFFFu, incl, l > 0 ? l - 1 : 0);
-                b = b0 + l;
-                base += l > 0 ? before : 0;
-                break;
-            }
-            base += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        bool found = false;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (!found && k * 32 < a.step.B) found = within(incl[k], k * 32);
+#pragma unroll 1
+        for (int b0 = kAhead * 32; !found && b0 < a.step.B; b0 += 32) found = within(warp_scan(sequence_cost(a, b0 + (threadIdx.x & 31))), b0);
+        return true;
+    }
+    __device__ __forceinline__ bool within(unsigned incl, int b0) {
+        const unsigned over = __ballot_sync(0xFFFFFFFFu, base + incl > pos);
+        if (over) {
+            const int l = __ffs(over) - 1;
+            const unsigned before = __shfl_sync(0xFFFFFFFFu, incl, l > 0 ? l - 1 : 0);
+            b = b0 + l;
+            base += l > 0 ? before : 0;
+            return true;
         }
+        base += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        return false;
     }
-    // The row tile of this CTA's last key tile (k0, k1: that tile alone).
-    __device__ bool last(const KvAttend& a, KvRun& r) {
-        pos = end - 1;
-        find(a, a.step.B <= 32 ? warp_scan(sequence_tiles(a, threadIdx.x & 31)) : 0);
-        return next(a, r);
+    // The CTA in whose share `at` lies: an estimate, put right.
+    __device__ __forceinline__ int owner(unsigned at) const {
+        int c = min((int)((float)at * ((float)grid / (float)total)), grid - 1);
+        while (begins(c) > at) --c;
+        while (c + 1 < grid && begins(c + 1) <= at) ++c;
+        return c;
     }
-    __device__ __forceinline__ int owner(long long tile) const { return (int)(((tile + 1) * grid - 1) / total); }
-    // The next run; false at the end.
-    __device__ bool next(const KvAttend& a, KvRun& r) {
-        if (pos >= end) return false;
+    // The row tile that holds pos: its run but for [k0, k1), its cost, its key tiles, and where it begins.
+    __device__ __forceinline__ bool row_tile(const KvAttend& a, KvRun& r, int& cost, int& n, unsigned& from) {
         int len, tokens;
-        long long per_head;
+        unsigned per_head;
+#pragma unroll 1
         for (;; ++b) {
-            if (b >= a.step.B) return false;                 // (cannot happen: the tiles were counted)
-            per_head = kv_sequence(a.shape, a.step, b, len, tokens, a.status) ? head_tiles(a, len, tokens) : 0;
+            if (b >= a.step.B) return false;                 // (pos is the end of everything)
+            per_head = kv_sequence(a.shape, a.step, b, len, tokens, a.status) ? head_cost(a, len, tokens) : 0;
             if (pos < base + per_head * a.shape.kv_heads) break;
             base += per_head * a.shape.kv_heads;
         }
-        long long off = pos - base;
+        unsigned off = pos - base;
         r.h = (int)(off / per_head);
         off -= r.h * per_head;
         r.rt = 0;
-        int n = tiles_of(a, len, tokens, 0);
-        if (a.step.mask) { r.rt = (int)(off / n); off -= (long long)r.rt * n; }
-        else while (off >= n) { off -= n; n = tiles_of(a, len, tokens, ++r.rt); }
+        n = tiles_of(a, len, tokens, 0);
+        if (a.step.mask) {
+            r.rt = min((int)(off / (unsigned)(kMost * n)), row_tiles(a, tokens) - 1);
+            off -= (unsigned)r.rt * (kMost * n);
+            cost = cost_of(a, tokens, r.rt);
+        } else {
+#pragma unroll 1
+            for (cost = cost_of(a, tokens, 0); off >= (unsigned)(n * cost); cost = cost_of(a, tokens, r.rt)) {
+                off -= n * cost;
+                n = tiles_of(a, len, tokens, ++r.rt);
+            }
+        }
+        from = pos - off;
         r.b = b; r.len = len; r.tokens = tokens;
         r.keys = keys_of(a, len, tokens, r.rt);
-        r.k0 = (int)off;
-        r.k1 = (int)min((long long)n, off + (end - pos));
-        const bool whole = r.k0 == 0 && r.k1 == n;
-        r.first = whole ? cta : owner(pos - off);
-        r.last = whole ? cta : owner(pos - off + n - 1);
-        pos += r.k1 - r.k0;
+        const unsigned last = from + (n - 1) * cost;
+        r.first = from >= begins(cta) ? cta : owner(from);
+        r.last = last < end ? cta : owner(last);
         return true;
     }
+    // The next run; false at the end.
+    __device__ __forceinline__ bool next(const KvAttend& a, KvRun& r) {
+#pragma unroll 1
+        while (pos < end) {
+            int cost, n;
+            unsigned from;
+            if (!row_tile(a, r, cost, n, from)) return false;
+            r.k0 = kHalves && cost == 2 ? (int)(pos - from + 1) >> 1 : (int)(pos - from);
+            r.k1 = min(n, kHalves && cost == 2 ? (int)(end - from + 1) >> 1 : (int)(end - from));
+            pos = from + n * cost;
+            if (r.k0 < r.k1) return true;
+        }
+        return false;
+    }
 };
+// What a call's costs stay below; the host refuses calls for which this does not fit in 31 bits.
+inline long long kv_cost_bound(const KvShape& s, int B, int T, int rows, int keys) {
+    const long long tiles = (((long long)s.max_pages << s.page_shift) + keys - 1) / keys, row_tiles = ((long long)T * (s.q_heads / s.kv_heads) + rows - 1) / rows;
+    return 2 * B * s.kv_heads * tiles * row_tiles;
+}
 
 // NaN codes of a step's values are taken as zero by the tensor-core kernels, which would otherwise spread them to rows that do not
 // see the token (0 * NaN); outputs that do see one are made NaN here, after they have been stored: elements [d, d + n) of query row
 // `row`.
 template <int D, class T>
-__device__ __noinline__ void kv_mark_nan(const KvAttend& a, const KvRun& r, int row, int d, int n) {
+__device__ __forceinline__ void kv_mark_nan(const KvAttend& a, const KvRun& r, int row, int d, int n) {
     const int token = (int)a.by_group.div((unsigned)row), hq = r.h * a.group + row - token * a.group;
     uint16_t* to = const_cast<uint16_t*>(a.out.data) + r.b * a.out.batch + token * a.out.token + hq * a.out.head;
 #pragma unroll 1
@@ -240,37 +289,46 @@ __device__ __forceinline__ bool kv_last_part(int* arrived, int pieces, int* word
 // slot to the next.  row0: the tile's first row.
 template <int kRows, int D, class T>
 __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
-    constexpr int kFloats = kv_part_floats<kRows, D>(), N = D / 32;
+    constexpr int kFloats = kv_part_floats<kRows, D>(), N = D / 32, kAtOnce = 8;       // parts in flight
     const int lane = threadIdx.x & 31, pieces = r.last - r.first + 1;
     const long long step = (long long)kStep * kFloats;
     auto part = [&](int i) { return parts + kv_slot(r, r.first + i) * step; };
     int seen = 0;
-    for (int i = lane; i < pieces; i += 32) seen |= __ldcg(reinterpret_cast<const int*>(part(i)) + kRows * D + 2 * kRows);
+    for (int i = lane; i < pieces; i += 32) seen |= reinterpret_cast<const int*>(part(i))[kRows * D + 2 * kRows];
     const bool nan = __any_sync(0xFFFFFFFFu, seen != 0);
+#pragma unroll 1
     for (int row = warp; row < rows; row += warps) {
         float top = -INFINITY, l = 0.f, x[N];
-        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, __ldcg(part(i) + kRows * D + row));
+        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, part(i)[kRows * D + row]);
         top = warp_max_f32(top);
         if (top == -INFINITY) top = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = 0.f;
+#pragma unroll 1
         for (int i0 = 0; i0 < pieces; i0 += 32) {
             float w = 0.f;
             if (i0 + lane < pieces) {
-                w = ex2_approx(__ldcg(part(i0 + lane) + kRows * D + row) - top);
-                l += w * __ldcg(part(i0 + lane) + kRows * D + kRows + row);
+                const float* at = part(i0 + lane) + kRows * D + row;
+                w = ex2_approx(at[0] - top);
+                l += w * at[kRows];
             }
             const int n = min(32, pieces - i0);
-#pragma unroll 8
-            for (int i = 0; i < n; ++i) {
-                const float f = __shfl_sync(0xFFFFFFFFu, w, i);
-                const float* at = part(i0 + i) + row * D + lane * N;
-                if (N == 4) {
-                    const float4 y = __ldcg(reinterpret_cast<const float4*>(at));
-                    x[0] += f * y.x; x[1] += f * y.y; x[2 % N] += f * y.z; x[3 % N] += f * y.w;
-                } else {
-                    const float2 y = __ldcg(reinterpret_cast<const float2*>(at));
-                    x[0] += f * y.x; x[1] += f * y.y;
+#pragma unroll 1
+            for (int i = 0; i < n; i += kAtOnce) {
+                float y[kAtOnce][N];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {                    // (parts behind the last are read again, with weight 0)
+                    const float* at = part(min(i0 + i + k, pieces - 1)) + row * D + lane * N;
+                    if (N == 4) *reinterpret_cast<float4*>(y[k]) = *reinterpret_cast<const float4*>(at);
+                    else *reinterpret_cast<float2*>(y[k]) = *reinterpret_cast<const float2*>(at);
+                }
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const float f = __shfl_sync(0xFFFFFFFFu, w, i + k);
+                    if (i + k < n) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[e] += f * y[k][e];
+                    }
                 }
             }
         }

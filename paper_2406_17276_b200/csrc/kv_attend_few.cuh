@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
     mbar_fence_init();
     __syncwarp();
     grid_dependency_wait();
-    KvWalk<kRows, kFewKeys> walk;
+    KvWalk<kRows, kFewKeys, false> walk;
     if (!walk.begin(a, blockIdx.x, gridDim.x)) return;
     KvRun r;
     uint32_t count = 0;                                      // blocks this warp has consumed: its place in the ring

@@ -25,7 +25,12 @@
 
 namespace ot {
 
-constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 14 * 32;
+// Registers a thread of each role; together they are what a block of five warpgroups is launched with (kRegsLaunch each, which the host
+// checks), or the warps that ask for more would wait for good.  (The kernel calls no function: with calls the compiler cannot keep to them.)
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 144, kRegsConvert = 64, kRegsIssue = 64;
+static_assert(2 * kRegsSoftmax + 2 * kRegsConvert + kRegsIssue <= 5 * kRegsLaunch, "registers of a block");
+
+constexpr int kTileRows = 128, kTileKeys = 128, kTileThreads = 20 * 32;
 
 // --- tcgen05 ---
 __device__ __forceinline__ void tmem_alloc(uint32_t* smem_word, uint32_t columns) {
@@ -121,7 +126,7 @@ template <int D> struct TileLayout {
            kBarO = kBarP + 4, kBarRKFull = kBarO + 4, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
            kBarEnd = kBarRVFree + kRaw, kBarCount };
     static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16;
-    static constexpr int kBytes = kMerge + 1024 + 1024;         // the base is brought to a multiple of 1024
+    static constexpr int kBytes = kMerge + 1024 + 16;
     static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
 };
 static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
@@ -164,14 +169,18 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {         /
 template <int D, class T>
 __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const __grid_constant__ KvAttend a) {
     using L = TileLayout<D>;
-    extern __shared__ unsigned char raw_smem[];
-    unsigned char* smem = raw_smem + ((1024u - (smem_u32(raw_smem) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) unsigned char tile_smem[];
+    unsigned char* smem = tile_smem;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + L::kBars);
     TileInfo* infos = reinterpret_cast<TileInfo*>(smem + L::kInfo);
     int* nans = reinterpret_cast<int*>(smem + L::kNan);
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + L::kWord);
-    if (warp == 12) {
+    if (smem_u32(smem) & 1023u) {                            // (swizzled operands need it; nothing has been started yet)
+        if (threadIdx.x == 0) set_status(a.status, kErrInternal);
+        return;
+    }
+    if (warp == 16) {
         if (lane == 0) {
             mbar_init(bars + L::kBarQ, 8);
             for (int i = 0; i < 2; ++i) {
@@ -200,12 +209,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     // counters stay in step and the kernel ends.
     bool dead = false;
     auto wait = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_warp(bars + bar, parity, a.status); };
-    KvWalk<2 * kTileRows, kTileKeys> walk;
+    KvWalk<2 * kTileRows, kTileKeys, true> walk;
     KvRun r;
     const bool any = walk.begin(a, blockIdx.x, gridDim.x);
     if (!any) {
     } else if (warp < 8) {
         // ---- softmax: a thread a row ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int X = warp >> 2, in_tile = threadIdx.x & 127;
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) * 32u << 16);
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
@@ -357,37 +367,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + (single ? 0 : X)) * kFloats;
             const bool nan = nans[run & (kTileSlots - 1)] != 0;
             ++run;
-            // a single row tile: the second group hands its sums to the first, over the queries, whose products are done
+            // a single row tile: the first group takes the second's sums, and reads its outputs from TMEM
+            const bool both = single && r.k1 - r.k0 > 1;
             float mine_f = ref, other_f = 0.f;
-            float* hand = reinterpret_cast<float*>(smem + L::kQ);                  // [128][D], chunks of four swizzled by row
-            float* hand_ml = reinterpret_cast<float*>(smem + L::kMerge);           // [2][128]
+            float* hand = reinterpret_cast<float*>(smem + L::kMerge);              // [2][128], and one
             if (single) {
                 if (X == 1) {
-                    if (mine && has) {
-                        hand_ml[in_tile] = m; hand_ml[128 + in_tile] = l;
-                    } else {
-                        hand_ml[in_tile] = -INFINITY; hand_ml[128 + in_tile] = 0.f;
-                    }
-                    if (busy && has) {
-#pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            float o[32];
-                            tmem_load(to + c * 32, o);
-                            tmem_wait(o);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                *reinterpret_cast<float4*>(hand + in_tile * D + (((c * 8 + i) ^ (in_tile & (D / 4 - 1))) << 2)) =
-                                    make_float4(o[4 * i] * ref, o[4 * i + 1] * ref, o[4 * i + 2] * ref, o[4 * i + 3] * ref);
-                        }
-                    }
+                    hand[in_tile] = m; hand[128 + in_tile] = l;
+                    if (in_tile == 0) hand[256] = ref;
+                    tc_fence_before();
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (X == 0) {
-                    const float m1 = hand_ml[in_tile], mm = fmaxf(m, m1), base = mm == -INFINITY ? 0.f : mm;
-                    const float f0 = ex2_approx(m - base);
-                    other_f = ex2_approx(m1 - base);
-                    l = l * f0 + hand_ml[128 + in_tile] * other_f;
-                    mine_f = ref * f0;
+                tc_fence_after();
+                if (both && X == 0) {
+                    const float m1 = hand[in_tile], mm = fmaxf(m, m1), base = mm == -INFINITY ? 0.f : mm;
+                    const float w0 = ex2_approx(m - base), w1 = ex2_approx(m1 - base);
+                    l = l * w0 + hand[128 + in_tile] * w1;
+                    mine_f = ref * w0;
+                    other_f = hand[256] * w1;
                     m = mm;
                 }
             }
@@ -401,14 +398,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     tmem_wait(x);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] *= mine_f;
-                    if (!mine) continue;
-                    if (single && r.k1 - r.k0 > 1) {
+                    if (both) {
+                        float y[32];
+                        tmem_load(to + D + c * 32, y);
+                        tmem_wait(y);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 y = *reinterpret_cast<const float4*>(hand + in_tile * D + (((c * 8 + i) ^ (in_tile & (D / 4 - 1))) << 2));
-                            x[4 * i] += y.x * other_f; x[4 * i + 1] += y.y * other_f; x[4 * i + 2] += y.z * other_f; x[4 * i + 3] += y.w * other_f;
-                        }
+                        for (int i = 0; i < 32; ++i) x[i] = fmaf(y[i], other_f, x[i]);
                     }
+                    if (!mine) continue;
                     if (cut) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
@@ -422,80 +419,69 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 if (cut && in_tile == 0) reinterpret_cast<int*>(part)[kTileRows * D + 2 * kTileRows] = nan;
             }
             tc_fence_before();
-            if (single) asm volatile("bar.sync 1, 256;" ::: "memory");             // the queries' place is free again
+            if (single) asm volatile("bar.sync 1, 256;" ::: "memory");             // the second group's outputs have been read
         }
-    } else if (warp < 12) {
-        // ---- conversion: codes to half precision, in the layout of the products ----
+    } else if (warp < 16) {
+        // ---- conversion: codes to half precision, in the layout of the products; four warps a side ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConvert));
         constexpr int kLanes = D / 16, kAtOnce = 128 / kLanes, kIter = 128 / kAtOnce;   // 16 codes a lane; keys at once
-        const int tid = threadIdx.x - 256, sub = tid & (kLanes - 1), key = tid / kLanes;
+        const int tid = threadIdx.x & 127, side = warp >= 12, sub = tid & (kLanes - 1), key = tid / kLanes;
         uint32_t done = 0;                                   // key tiles converted so far
         int run = 0;
-        auto read = [&](int raw, int full, int free_, uint4 (&x)[kIter]) {       // a side's codes from their stage, which is free after that
-            const uint32_t st = done % L::kRaw, phase = done / L::kRaw & 1;
-            wait(full + st, phase);
-            const unsigned char* from = smem + raw + st * L::kCodes + tid * 16;
-#pragma unroll
-            for (int i = 0; i < kIter; ++i) x[i] = *reinterpret_cast<const uint4*>(from + i * 2048);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bars + free_ + st);
-        };
-        auto write = [&](unsigned char* to, const uint4 (&x)[kIter], const uint32_t (&ratio)[8]) {
-#pragma unroll
-            for (int i = 0; i < kIter; ++i) {
-                const int row = i * kAtOnce + key;
-                const uint32_t two_f = ratio[row >> 4];
-                const __half2 f = *reinterpret_cast<const __half2*>(&two_f);
-                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                uint32_t h[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t two = from_e4m3x2((uint16_t)(w[e >> 1] >> (e & 1) * 16));
-                    const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&two), f);
-                    h[e] = *reinterpret_cast<const uint32_t*>(&y);
-                }
-                // two chunks of eight elements; lanes of the second 64 elements begin with the other one, whose banks are free
-                const int block = sub >> 2, chunk = (sub & 3) * 2;
-                unsigned char* base = to + block * (128 * 128) + row * 128;
-                const uint4 c0 = make_uint4(h[0], h[1], h[2], h[3]), c1 = make_uint4(h[4], h[5], h[6], h[7]);
-                *reinterpret_cast<uint4*>(base + (((chunk + block) ^ (row & 7)) << 4)) = block ? c1 : c0;
-                *reinterpret_cast<uint4*>(base + (((chunk + 1 - block) ^ (row & 7)) << 4)) = block ? c0 : c1;
-            }
-        };
+        // where this lane's two chunks of eight elements go in a row; lanes of the second 64 elements begin with the other one, whose banks
+        // are free
+        const int block = sub >> 2, chunk = (sub & 3) * 2;
         while (walk.next(a, r)) {
             const int end = r.len + r.tokens;                // slots at or beyond it are not the sequence's
             for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
-                const uint32_t stage = done & 1, phase = done >> 1 & 1;
+                const uint32_t stage = done & 1, phase = done >> 1 & 1, st = done % L::kRaw, raw_phase = done / L::kRaw & 1;
                 const TileInfo& info = infos[done & (kTileSlots - 1)];
-                uint4 x[kIter];
-                read(L::kRawK, L::kBarRKFull, L::kBarRKFree, x);
-                wait(L::kBarKFree + stage, phase ^ 1);
-                write(smem + L::kK + stage * L::kOperand, x, info.kratio);
-                proxy_fence();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + L::kBarKFull + stage);
-                read(L::kRawV, L::kBarRVFull, L::kBarRVFree, x);
-                if ((kt + 1) * kTileKeys > r.len) {          // NaN codes of the step's own values, and what lies behind them
+                {
+                    const int raw_full = side ? L::kBarRVFull : L::kBarRKFull, raw_free = side ? L::kBarRVFree : L::kBarRKFree;
+                    const int full = side ? L::kBarVFull : L::kBarKFull, free_ = side ? L::kBarVFree : L::kBarKFree;
+                    const unsigned char* from = smem + (side ? L::kRawV : L::kRawK) + st * L::kCodes + tid * 16;
+                    unsigned char* to = smem + (side ? L::kV : L::kK) + stage * L::kOperand + block * (128 * 128);
+                    const uint32_t* ratios = side ? info.vratio : info.kratio;
+                    const bool edge = side && (kt + 1) * kTileKeys > r.len;        // NaN codes of the step's own values, and what lies behind them
                     uint32_t seen = 0;
-#pragma unroll
+                    wait(raw_full + st, raw_phase);
+                    wait(free_ + stage, phase ^ 1);
+#pragma unroll 2
                     for (int i = 0; i < kIter; ++i) {
-                        const int s = kt * kTileKeys + i * kAtOnce + key;
-                        if (s >= end) x[i] = make_uint4(0, 0, 0, 0);
-                        else if (s >= r.len) {
-                            x[i].x = drop_nan(x[i].x, seen); x[i].y = drop_nan(x[i].y, seen);
-                            x[i].z = drop_nan(x[i].z, seen); x[i].w = drop_nan(x[i].w, seen);
+                        const int row = i * kAtOnce + key;
+                        uint4 x = *reinterpret_cast<const uint4*>(from + i * 2048);
+                        if (edge) {
+                            const int s = kt * kTileKeys + row;
+                            if (s >= end) x = make_uint4(0, 0, 0, 0);
+                            else if (s >= r.len) { x.x = drop_nan(x.x, seen); x.y = drop_nan(x.y, seen); x.z = drop_nan(x.z, seen); x.w = drop_nan(x.w, seen); }
                         }
+                        const __half2 f = *reinterpret_cast<const __half2*>(ratios + (row >> 4));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t h[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t two = from_e4m3x2((uint16_t)(w[e >> 1] >> (e & 1) * 16));
+                            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&two), f);
+                            h[e] = *reinterpret_cast<const uint32_t*>(&y);
+                        }
+                        const uint4 c0 = make_uint4(h[0], h[1], h[2], h[3]), c1 = make_uint4(h[4], h[5], h[6], h[7]);
+                        *reinterpret_cast<uint4*>(to + row * 128 + (((chunk + block) ^ (row & 7)) << 4)) = block ? c1 : c0;
+                        *reinterpret_cast<uint4*>(to + row * 128 + (((chunk + 1 - block) ^ (row & 7)) << 4)) = block ? c0 : c1;
                     }
                     if (seen) atomicOr(nans + (run & (kTileSlots - 1)), 1);
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bars + raw_free + st);
+                        mbar_arrive(bars + full + stage);
+                    }
                 }
-                wait(L::kBarVFree + stage, phase ^ 1);
-                write(smem + L::kV + stage * L::kOperand, x, info.vratio);
-                proxy_fence();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + L::kBarVFull + stage);
             }
             ++run;
         }
-    } else if (warp == 13) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+    if (warp == 17) {
         // ---- copies: pages of a key tile, a lane for each 16 keys; four tiles are looked up at a time, four ahead ----
         uint32_t done = 0;
         int run = 0;
@@ -564,7 +550,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 mbar_wait_warp(bars + L::kBarRKFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
                 mbar_wait_warp(bars + L::kBarRVFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
             }
-    } else if (warp == 12) {
+    } else if (warp == 16) {
         // ---- products: one lane issues ----
         if (elect_one()) {
             constexpr uint32_t kScores = tc_idesc(64, false), kOutputs = tc_idesc(D, true), kHalf = 64 * 128 >> 4, kStageStep = L::kOperand >> 4;
@@ -589,55 +575,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 for (int k = 0; k < 4; ++k) tc_mma_ts(d, p + k * 8, v + k * (2048 >> 4), kOutputs, add || k > 0);
                 tc_commit(bars + L::kBarO + 2 * X + half);
             };
-            auto keys = [&](uint32_t tile) {                 // waits for a tile's keys
-                wait1(L::kBarKFull + (tile & 1), tile >> 1 & 1);
-                tc_fence_after();
-            };
             while (walk.next(a, r)) {
+                // Two row tiles in turn, each with its own scores; or one, whose key tiles the two groups take in turn.  A key tile's scores are
+                // issued `ahead` tiles before its values; both stand here once for all cases, for the sake of the instruction cache.
                 const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
-                const int n = r.k1 - r.k0;
+                const int n = r.k1 - r.k0, ahead = single ? 2 : 1, pieces = single ? 2 : 4;
                 wait1(L::kBarQ, nrun & 1);
                 ++nrun;
-                if (single) {                                // one row tile: the two groups take its key tiles in turn
-                    for (int i = 0; i < min(n, 2); ++i) {
-                        keys(done + i);
-                        for (int half = 0; half < 2; ++half) scores(i, 0, (done + i) & 1, half);
-                        tc_commit(bars + L::kBarKFree + ((done + i) & 1));
-                    }
-                    for (int i = 0; i < n; ++i, ++done) {
-                        const uint32_t stage = done & 1;
-                        wait1(L::kBarVFull + stage, done >> 1 & 1);
-                        for (int half = 0; half < 2; ++half) {
-                            outputs(i & 1, stage, half, i > 1 || half);
-                            if (i + 2 < n) {
-                                if (half == 0) keys(done + 2);
-                                scores(i & 1, 0, stage, half);
+#pragma unroll 1
+                for (int i = -ahead; i < n; ++i) {
+                    const uint32_t now = (done + i) & 1, tile = done + i + ahead, next = tile & 1;
+                    const bool more = i + ahead < n;
+                    if (i >= 0) wait1(L::kBarVFull + now, (done + i) >> 1 & 1);
+#pragma unroll 1
+                    for (int k = 0; k < pieces; ++k) {
+                        const int half = single ? k : k >> 1, X = single ? i & 1 : k & 1;
+                        if (i >= 0) outputs(X, now, half, i >= ahead || half);
+                        if (more) {
+                            if (k == 0) {
+                                wait1(L::kBarKFull + next, tile >> 1 & 1);
+                                tc_fence_after();
                             }
+                            scores(X, single ? 0 : X, next, half);
                         }
-                        tc_commit(bars + L::kBarVFree + stage);
-                        if (i + 2 < n) tc_commit(bars + L::kBarKFree + stage);
                     }
-                } else {                                     // two row tiles in turn
-                    keys(done);
-                    for (int half = 0; half < 2; ++half)
-                        for (int X = 0; X < 2; ++X) scores(X, X, done & 1, half);
-                    tc_commit(bars + L::kBarKFree + (done & 1));
-                    for (int i = 0; i < n; ++i, ++done) {
-                        const uint32_t stage = done & 1, next = (done + 1) & 1;
-                        const bool more = i + 1 < n;
-                        wait1(L::kBarVFull + stage, done >> 1 & 1);
-                        for (int half = 0; half < 2; ++half)
-                            for (int X = 0; X < 2; ++X) {
-                                outputs(X, stage, half, i > 0 || half);
-                                if (more) {
-                                    if (X == 0 && half == 0) keys(done + 1);
-                                    scores(X, X, next, half);
-                                }
-                            }
-                        tc_commit(bars + L::kBarVFree + stage);
-                        if (more) tc_commit(bars + L::kBarKFree + next);
-                    }
+                    if (i >= 0) tc_commit(bars + L::kBarVFree + now);
+                    if (more) tc_commit(bars + L::kBarKFree + next);
                 }
+                done += n;
             }
             // everything issued is complete before TMEM is given back, also after a wait that ran out
             tc_commit(bars + L::kBarEnd);
@@ -645,24 +610,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         }
         __syncwarp();
     }
+    }
+    // the cut row tile that begins here, for the kernel that joins the parts
+    if (warp == 8 && lane == 0) a.cuts[blockIdx.x] = any && r.first != r.last && r.first == (int)blockIdx.x ? r : KvRun{-1};
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_free(tmem, L::kColumns);
+    if (warp == 16) tmem_free(tmem, L::kColumns);
 }
 
-// Joins the parts of the row tiles that the kernel above has cut: block (c, j) takes rows j, j + kJoinBlocks, ... (of each eight) of the tile that
-// began in CTA c.  A kernel of its own, because there is much to read (64 KB a part at D = 128) and the CTA that finished last would be
+// Joins the parts of the row tiles that the kernel above has cut: block (c, j) takes eight rows of every 8 * kJoinBlocks of the tile that began
+// in CTA c, if it is one.  A kernel of its own, because there is much to read (64 KB a part at D = 128) and the CTA that finished last would be
 // alone with it.
 constexpr int kJoinBlocks = 16;
 
 template <int D, class T>
-__global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttend a, int grid) {
+__global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttend a) {
     grid_dependency_wait();
-    KvWalk<2 * kTileRows, kTileKeys> walk;
-    KvRun r;
-    if (!walk.begin(a, blockIdx.x, grid) || !walk.last(a, r)) return;
-    if (r.first == r.last || r.first != (int)blockIdx.x) return;
+    const KvRun r = a.cuts[blockIdx.x];
+    if (r.b < 0) return;
     constexpr int kFloats = kv_part_floats<kTileRows, D>();
     const int warp = threadIdx.x >> 5;
     for (int X = 0; X < 2; ++X) {
