@@ -99,7 +99,7 @@ struct KvWalk {
         }
         return v;
     }
-    __device__ __forceinline__ unsigned begins(int c) const { return share * c + left * c / grid; }       // total * c / grid
+    __device__ __forceinline__ unsigned begins(int c) const { return share * c + min((unsigned)c, left); }        // the first `left` CTAs have one more
     // false: nothing for this CTA.
     __device__ __forceinline__ bool begin(const KvAttend& a, int which, int ctas) {
         unsigned incl[kAhead];
@@ -146,12 +146,10 @@ struct KvWalk {
         base += __shfl_sync(0xFFFFFFFFu, incl, 31);
         return false;
     }
-    // The CTA in whose share `at` lies: an estimate, put right.
+    // The CTA in whose share `at` lies.
     __device__ __forceinline__ int owner(unsigned at) const {
-        int c = min((int)((float)at * ((float)grid / (float)total)), grid - 1);
-        while (begins(c) > at) --c;
-        while (c + 1 < grid && begins(c + 1) <= at) ++c;
-        return c;
+        const unsigned more = left * (share + 1);
+        return at < more ? (int)(at / (share + 1)) : (int)(left + (at - more) / share);
     }
     // The row tile that holds pos: its run but for [k0, k1), its cost, its key tiles, and where it begins.
     __device__ __forceinline__ bool row_tile(const KvAttend& a, KvRun& r, int& cost, int& n, unsigned& from) {
@@ -234,7 +232,8 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t four, uint32_t& seen) {
 }
 
 // A cut row tile's part: kRows x D unnormalised outputs (values' scales applied), then maxima, sums and a word that says whether
-// NaN values were met.
+// NaN values were met.  Outputs lie in chunks of four elements, [D / 4][kRows][4], so that threads with a row each write and read whole
+// lines (row after row, each store of a warp touched 32 lines, and writing a tile's part took as long as four key tiles).
 template <int kRows, int D> __host__ __device__ constexpr int kv_part_floats() { return kRows * D + 2 * kRows + 4; }
 
 // A row's outputs at elements [d, d + N) of query row `row` of the run (row tile included).
@@ -285,60 +284,59 @@ __device__ __forceinline__ bool kv_last_part(int* arrived, int pieces, int* word
     asm volatile("bar.sync %0, %1;" ::"n"(kBarrier), "n"(kThreadsN) : "memory");
     return *word != 0;
 }
-// Joins a cut row tile's parts in the order of the keys: a warp a row, for the rows warp, warp + warps, ... of it.  kStep: parts from one
-// slot to the next.  row0: the tile's first row.
+// Joins a cut row tile's parts in the order of the keys: a lane a row, a chunk of four elements at a time.  kStep: parts from one slot to
+// the next.  row0: the tile's first row.  Of the tile's groups of rows times chunks (kLanesOf lanes each) this warp does warp, warp + warps, ...
 template <int kRows, int D, class T>
 __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
-    constexpr int kFloats = kv_part_floats<kRows, D>(), N = D / 32, kAtOnce = 8;       // parts in flight
+    constexpr int kFloats = kv_part_floats<kRows, D>(), kChunks = D / 4, kAtOnce = 8;      // parts in flight
+    constexpr int kLaneRows = kRows < 32 ? kRows : 32, kLaneChunks = 32 / kLaneRows;
     const int lane = threadIdx.x & 31, pieces = r.last - r.first + 1;
     const long long step = (long long)kStep * kFloats;
-    auto part = [&](int i) { return parts + kv_slot(r, r.first + i) * step; };
+    auto part = [&](int i) { return parts + kv_slot(r, r.first + min(i, pieces - 1)) * step; };
     int seen = 0;
     for (int i = lane; i < pieces; i += 32) seen |= reinterpret_cast<const int*>(part(i))[kRows * D + 2 * kRows];
     const bool nan = __any_sync(0xFFFFFFFFu, seen != 0);
+    constexpr int kItems = (kRows / kLaneRows) * (kChunks / kLaneChunks);
 #pragma unroll 1
-    for (int row = warp; row < rows; row += warps) {
-        float top = -INFINITY, l = 0.f, x[N];
-        for (int i = lane; i < pieces; i += 32) top = fmaxf(top, part(i)[kRows * D + row]);
-        top = warp_max_f32(top);
-        if (top == -INFINITY) top = 0.f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = 0.f;
+    for (int item = warp; item < kItems; item += warps) {
+        const int row = item / (kChunks / kLaneChunks) * kLaneRows + lane % kLaneRows, chunk = item % (kChunks / kLaneChunks) * kLaneChunks + lane / kLaneRows;
+        if (item / (kChunks / kLaneChunks) * kLaneRows >= rows) break;
+        float top = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-        for (int i0 = 0; i0 < pieces; i0 += 32) {
-            float w = 0.f;
-            if (i0 + lane < pieces) {
-                const float* at = part(i0 + lane) + kRows * D + row;
-                w = ex2_approx(at[0] - top);
-                l += w * at[kRows];
-            }
-            const int n = min(32, pieces - i0);
-#pragma unroll 1
-            for (int i = 0; i < n; i += kAtOnce) {
-                float y[kAtOnce][N];
+        for (int i = 0; i < pieces; i += kAtOnce) {
+            float m[kAtOnce];
 #pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {                    // (parts behind the last are read again, with weight 0)
-                    const float* at = part(min(i0 + i + k, pieces - 1)) + row * D + lane * N;
-                    if (N == 4) *reinterpret_cast<float4*>(y[k]) = *reinterpret_cast<const float4*>(at);
-                    else *reinterpret_cast<float2*>(y[k]) = *reinterpret_cast<const float2*>(at);
-                }
+            for (int k = 0; k < kAtOnce; ++k) m[k] = part(i + k)[kRows * D + row];
 #pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const float f = __shfl_sync(0xFFFFFFFFu, w, i + k);
-                    if (i + k < n) {
-#pragma unroll
-                        for (int e = 0; e < N; ++e) x[e] += f * y[k][e];
-                    }
-                }
-            }
+            for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
         }
+        if (top == -INFINITY) top = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < pieces; i += kAtOnce) {
+            float m[kAtOnce], s[kAtOnce];
+            float4 y[kAtOnce];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+            for (int k = 0; k < kAtOnce; ++k) {                        // (parts behind the last are read again, with weight 0)
+                const float* at = part(i + k);
+                m[k] = at[kRows * D + row];
+                s[k] = at[kRows * D + kRows + row];
+                y[k] = *reinterpret_cast<const float4*>(at + (chunk * kRows + row) * 4);
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (i + k < pieces) {
+                    const float f = ex2_approx(m[k] - top);
+                    l += f * s[k];
+                    x[0] += f * y[k].x; x[1] += f * y[k].y; x[2] += f * y[k].z; x[3] += f * y[k].w;
+                }
+        }
         const float f = 1.f / l;
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] *= f;
-        kv_store<D, N, T>(a, r, row0 + row, lane * N, x, nan);
-        if (lane == 0) kv_store_lse(a, r, row0 + row, top, l);
+        for (int e = 0; e < 4; ++e) x[e] *= f;
+        if (row < rows) {
+            kv_store<D, 4, T>(a, r, row0 + row, chunk * 4, x, nan);
+            if (chunk == 0) kv_store_lse(a, r, row0 + row, top, l);
+        }
     }
 }
 

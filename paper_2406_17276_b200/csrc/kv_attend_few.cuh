@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
                 sum.x += f * y.x; sum.y += f * y.y; sum.z += f * y.z; sum.w += f * y.w;
             }
             if (cut) {
-                *reinterpret_cast<float4*>(part + row * D + d) = sum;
+                *reinterpret_cast<float4*>(part + (d / 4 * kRows + row) * 4) = sum;
                 if (d == 0) { part[kRows * D + row] = mm; part[kRows * D + kRows + row] = ll; }
             } else {
                 const float f = 1.f / ll;

@@ -112,7 +112,7 @@ struct TileInfo {
     float kmax, ref;                     // largest scale of the keys, reference of the values
     float pad[2];
 };
-// Slots of TileInfo, by tile, and of the NaN word, by run.  The copying warp writes those of tile t (of run r) once the codes of tile t - 2 at
+// Slots of TileInfo, by tile, and of the runs and their NaN words, by run.  The copying warp writes those of tile t (of run r) once the codes of tile t - 2 at
 // least have been taken; then values of t - 3 have been written, so the products of t - 5 are complete, so both softmax groups are done with
 // tile t - 5, and done with the run before that tile's.
 constexpr int kTileSlots = 8;
@@ -124,9 +124,11 @@ template <int D> struct TileLayout {
     static constexpr int kBars = kRawV + kRaw * kCodes;
     enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 4,
            kBarO = kBarP + 4, kBarRKFull = kBarO + 4, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
-           kBarEnd = kBarRVFree + kRaw, kBarCount };
-    static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16;
-    static constexpr int kBytes = kMerge + 1024 + 16;
+           kBarRun = kBarRVFree + kRaw,
+           kBarEnd = kBarRun + kTileSlots, kBarCount };
+    static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16,
+                         kRuns = kMerge + 1024 + 16;
+    static constexpr int kBytes = kRuns + kTileSlots * (int)sizeof(KvRun);
     static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
 };
 static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
@@ -175,6 +177,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem + L::kBars);
     TileInfo* infos = reinterpret_cast<TileInfo*>(smem + L::kInfo);
     int* nans = reinterpret_cast<int*>(smem + L::kNan);
+    KvRun* runs = reinterpret_cast<KvRun*>(smem + L::kRuns);
     uint32_t* words = reinterpret_cast<uint32_t*>(smem + L::kWord);
     if (smem_u32(smem) & 1023u) {                            // (swizzled operands need it; nothing has been started yet)
         if (threadIdx.x == 0) set_status(a.status, kErrInternal);
@@ -194,6 +197,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 mbar_init(bars + L::kBarRKFull + i, 1); mbar_init(bars + L::kBarRKFree + i, 4);
                 mbar_init(bars + L::kBarRVFull + i, 1); mbar_init(bars + L::kBarRVFree + i, 4);
             }
+            for (int i = 0; i < kTileSlots; ++i) mbar_init(bars + L::kBarRun + i, 1);
             mbar_init(bars + L::kBarEnd, 1);
             mbar_fence_init();
         }
@@ -209,11 +213,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     // counters stay in step and the kernel ends.
     bool dead = false;
     auto wait = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_warp(bars + bar, parity, a.status); };
-    KvWalk<2 * kTileRows, kTileKeys, true> walk;
     KvRun r;
-    const bool any = walk.begin(a, blockIdx.x, gridDim.x);
-    if (!any) {
-    } else if (warp < 8) {
+    // the next run of this CTA, from the copying warp; false at the end
+    int runs_taken = 0;
+    auto next_run = [&](auto&& waits) {
+        const int slot = runs_taken & (kTileSlots - 1);
+        waits(L::kBarRun + slot, runs_taken / kTileSlots & 1);
+        ++runs_taken;
+        r = runs[slot];
+        return !dead && r.b >= 0;
+    };
+    if (warp < 8) {
         // ---- softmax: a thread a row ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int X = warp >> 2, in_tile = threadIdx.x & 127;
@@ -221,7 +231,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
         uint32_t tiles = 0, at = 0;                          // key tiles of this group, and of the runs before
         int run = 0;
-        while (walk.next(a, r)) {
+        while (next_run(wait)) {
             const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
             const int row0 = r.rt * 2 * kTileRows + (single ? 0 : X * kTileRows), rows = min(kTileRows, r.tokens * a.group - row0);
             const int row = row0 + in_tile;
@@ -231,42 +241,41 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             // elements below 2^-22 of the row's largest)
             float qf = a.scale;
             {
-                uint4 q[D / 8];
-                if (mine) {
-                    const int hq = r.h * a.group + row - token * a.group;
-                    const uint16_t* from = a.q.data + r.b * a.q.batch + token * a.q.token + hq * a.q.head;
+                constexpr int kRowLanes = D / 8, kAt = 32 / kRowLanes, kLoads = 32 / kAt;          // rows at once; all of a warp's 32 in flight
+                const int sub = lane & (kRowLanes - 1), low = (warp & 3) * 32;
+                uint4 q[kLoads];
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) q[i] = load8(from + i * 8, a.wide_q);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) q[i] = make_uint4(0, 0, 0, 0);
-                }
-                float f = 1.f;
-                if (!std::is_same<T, __half>::value) {
-                    uint32_t top = 0;
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, w[e] >> 16 & 0x7FFFu));
+                for (int i = 0; i < kLoads; ++i) {
+                    const int at_row = low + i * kAt + lane / kRowLanes;
+                    q[i] = make_uint4(0, 0, 0, 0);
+                    if (at_row < rows) {
+                        const int tok = (int)a.by_group.div((unsigned)(row0 + at_row)), hq = r.h * a.group + row0 + at_row - tok * a.group;
+                        q[i] = load8(a.q.data + r.b * a.q.batch + tok * a.q.token + hq * a.q.head + sub * 8, a.wide_q);
                     }
-                    const int e = min(max((int)(top >> 7) - 127, -112), 120);
-                    f = power_of_two(8 - e);
-                    qf *= power_of_two(e - 8);
                 }
-                if (!single || X == 0) {
-                    unsigned char* to_q = smem + L::kQ + X * L::kOperand + in_tile * 128;
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                        uint32_t h[4];
+                for (int i = 0; i < kLoads; ++i) {
+                    const int at_row = low + i * kAt + lane / kRowLanes;
+                    uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    if (!std::is_same<T, __half>::value) {
+                        uint32_t top = 0;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float2 y = to_float2<T>(w[e]);
-                            h[e] = std::is_same<T, __half>::value ? w[e] : from_float2<__half>(y.x * f, y.y * f);
+                        for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7FFFu, w[k] >> 16 & 0x7FFFu));
+#pragma unroll
+                        for (int o = kRowLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                        const int e = min(max((int)(top >> 7) - 127, -112), 120) - 8;
+                        const int own = __shfl_sync(0xFFFFFFFFu, e, lane % kAt * kRowLanes);       // this thread's row, if it is among these
+                        if (lane / kAt == i) qf = a.scale * power_of_two(own);
+                        const float f = power_of_two(-e);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float2 y = to_float2<T>(w[k]);
+                            w[k] = from_float2<__half>(y.x * f, y.y * f);
                         }
-                        *reinterpret_cast<uint4*>(to_q + (i >> 3) * (128 * 128) + (((i & 7) ^ (in_tile & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                     }
+                    if (!single || X == 0)
+                        *reinterpret_cast<uint4*>(smem + L::kQ + X * L::kOperand + (sub >> 3) * (128 * 128) + at_row * 128 + (((sub & 7) ^ (at_row & 7)) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
             proxy_fence();
@@ -409,7 +418,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     if (cut) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            *reinterpret_cast<float4*>(part + in_tile * D + c * 32 + i * 4) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                            *reinterpret_cast<float4*>(part + ((c * 8 + i) * kTileRows + in_tile) * 4) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
                     } else {
                         kv_store<D, 32, T>(a, r, row, c * 32, x, nan);
                     }
@@ -431,7 +440,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         // where this lane's two chunks of eight elements go in a row; lanes of the second 64 elements begin with the other one, whose banks
         // are free
         const int block = sub >> 2, chunk = (sub & 3) * 2;
-        while (walk.next(a, r)) {
+        while (next_run(wait)) {
             const int end = r.len + r.tokens;                // slots at or beyond it are not the sequence's
             for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
                 const uint32_t stage = done & 1, phase = done >> 1 & 1, st = done % L::kRaw, raw_phase = done / L::kRaw & 1;
@@ -487,7 +496,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         int run = 0;
         const int shift = a.shape.page_shift, inside = a.shape.page - 1;
         const int copy_rows = min(a.shape.page, kTileKeys);
-        while (walk.next(a, r)) {
+        KvWalk<2 * kTileRows, kTileKeys, true> walk;
+        KvRun before{-1};
+        bool more = walk.begin(a, blockIdx.x, gridDim.x);
+        for (int given = 0;; ++given) {
+            more = more && walk.next(a, r) && !dead;
+            if (!more) r.b = -1;
+            if (lane == 0) {
+                runs[given & (kTileSlots - 1)] = r;
+                mbar_arrive(bars + L::kBarRun + (given & (kTileSlots - 1)));
+            }
+            __syncwarp();
+            if (!more) break;
+            before = r;
             const int end = r.len + r.tokens;
             int id[2];
             float ks[2], vs[2];
@@ -544,6 +565,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             }
             ++run;
         }
+        // the cut row tile that begins here, for the kernel that joins the parts
+        if (lane == 0) {
+            if (before.first == before.last || before.first != (int)blockIdx.x) before.b = -1;
+            a.cuts[blockIdx.x] = before;
+        }
         // copies in flight land before the CTA ends, also where their reader has given up
         for (uint32_t i = 0; i < L::kRaw; ++i)
             if (dead && done > i) {
@@ -575,7 +601,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 for (int k = 0; k < 4; ++k) tc_mma_ts(d, p + k * 8, v + k * (2048 >> 4), kOutputs, add || k > 0);
                 tc_commit(bars + L::kBarO + 2 * X + half);
             };
-            while (walk.next(a, r)) {
+            while (next_run(wait1)) {
                 // Two row tiles in turn, each with its own scores; or one, whose key tiles the two groups take in turn.  A key tile's scores are
                 // issued `ahead` tiles before its values; both stand here once for all cases, for the sake of the instruction cache.
                 const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
@@ -611,8 +637,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         __syncwarp();
     }
     }
-    // the cut row tile that begins here, for the kernel that joins the parts
-    if (warp == 8 && lane == 0) a.cuts[blockIdx.x] = any && r.first != r.last && r.first == (int)blockIdx.x ? r : KvRun{-1};
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
