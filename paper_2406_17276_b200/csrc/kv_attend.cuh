@@ -288,7 +288,7 @@ __device__ __forceinline__ bool kv_last_part(int* arrived, int pieces, int* word
 // the next.  row0: the tile's first row.  Of the tile's groups of rows times chunks (kLanesOf lanes each) this warp does warp, warp + warps, ...
 template <int kRows, int D, class T>
 __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
-    constexpr int kFloats = kv_part_floats<kRows, D>(), kChunks = D / 4, kAtOnce = 8;      // parts in flight
+    constexpr int kFloats = kv_part_floats<kRows, D>(), kChunks = D / 4, kAtOnce = kRows < 32 ? 16 : 8;      // parts in flight
     constexpr int kLaneRows = kRows < 32 ? kRows : 32, kLaneChunks = 32 / kLaneRows;
     const int lane = threadIdx.x & 31, pieces = r.last - r.first + 1;
     const long long step = (long long)kStep * kFloats;
@@ -304,15 +304,6 @@ __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const
         float top = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
         for (int i = 0; i < pieces; i += kAtOnce) {
-            float m[kAtOnce];
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) m[k] = part(i + k)[kRows * D + row];
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
-        }
-        if (top == -INFINITY) top = 0.f;
-#pragma unroll 1
-        for (int i = 0; i < pieces; i += kAtOnce) {
             float m[kAtOnce], s[kAtOnce];
             float4 y[kAtOnce];
 #pragma unroll
@@ -322,14 +313,22 @@ __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const
                 s[k] = at[kRows * D + kRows + row];
                 y[k] = *reinterpret_cast<const float4*>(at + (chunk * kRows + row) * 4);
             }
+            const float was = top;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
+            const float bottom = top == -INFINITY ? 0.f : top, fade = ex2_approx(was - bottom);
+            l *= fade;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] *= fade;
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
                 if (i + k < pieces) {
-                    const float f = ex2_approx(m[k] - top);
+                    const float f = ex2_approx(m[k] - bottom);
                     l += f * s[k];
                     x[0] += f * y[k].x; x[1] += f * y[k].y; x[2] += f * y[k].z; x[3] += f * y[k].w;
                 }
         }
+        if (top == -INFINITY) top = 0.f;
         const float f = 1.f / l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] *= f;
