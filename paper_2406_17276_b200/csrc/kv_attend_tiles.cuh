@@ -237,45 +237,66 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             const int row = row0 + in_tile;
             const bool mine = in_tile < rows, busy = (warp & 3) * 32 < rows;       // this thread, this warp
             const int token = (int)a.by_group.div((unsigned)min(row, r.tokens * a.group - 1));
-            // queries to shared memory; bf16 rows are brought to half precision by a power of two of their own (exact but for
-            // elements below 2^-22 of the row's largest)
+            // Queries to shared memory, D / 8 lanes a row, all of a warp's 32 rows in flight.  bf16 numbers from 2^-17 on to 2^15 are half-precision
+            // numbers too; where a row is larger, or has nothing above 2^-6, the warp's rows are brought there by powers of two of
+            // their own (exact but for elements below 2^-22 of the row's largest).
             float qf = a.scale;
             {
-                constexpr int kRowLanes = D / 8, kAt = 32 / kRowLanes, kLoads = 32 / kAt;          // rows at once; all of a warp's 32 in flight
+                constexpr int kRowLanes = D / 8, kAt = 32 / kRowLanes, kLoads = 32 / kAt;
+                constexpr uint32_t kRowMask = kRowLanes == 16 ? 0xFFFFu : 0xFFu;
                 const int sub = lane & (kRowLanes - 1), low = (warp & 3) * 32;
-                uint4 q[kLoads];
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
+                unsigned char* to_q = smem + L::kQ + X * L::kOperand + (sub >> 3) * (128 * 128);
+                auto fetch = [&](int i) {
                     const int at_row = low + i * kAt + lane / kRowLanes;
-                    q[i] = make_uint4(0, 0, 0, 0);
-                    if (at_row < rows) {
-                        const int tok = (int)a.by_group.div((unsigned)(row0 + at_row)), hq = r.h * a.group + row0 + at_row - tok * a.group;
-                        q[i] = load8(a.q.data + r.b * a.q.batch + tok * a.q.token + hq * a.q.head + sub * 8, a.wide_q);
+                    if (at_row >= rows) return make_uint4(0, 0, 0, 0);
+                    const int tok = (int)a.by_group.div((unsigned)(row0 + at_row)), hq = r.h * a.group + row0 + at_row - tok * a.group;
+                    return load8(a.q.data + r.b * a.q.batch + tok * a.q.token + hq * a.q.head + sub * 8, a.wide_q);
+                };
+                auto magnitude = [&](const uint4& q) {       // largest of the lane's eight, as a bf16 pattern
+                    const uint32_t m2 = max_bf16x2(max_bf16x2(q.x & 0x7FFF7FFFu, q.y & 0x7FFF7FFFu), max_bf16x2(q.z & 0x7FFF7FFFu, q.w & 0x7FFF7FFFu));
+                    return max(m2 & 0xFFFFu, m2 >> 16);
+                };
+                auto keep = [&](int i, const uint4& q, float f) {
+                    const int at_row = low + i * kAt + lane / kRowLanes;
+                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+                    uint32_t h[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 y = to_float2<T>(w[k]);
+                        h[k] = std::is_same<T, __half>::value ? w[k] : from_float2<__half>(y.x * f, y.y * f);
+                    }
+                    if (!single || X == 0) *reinterpret_cast<uint4*>(to_q + at_row * 128 + (((sub & 7) ^ (at_row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                };
+                uint4 q[kLoads];
+                bool fits = true;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) q[i] = fetch(i);
+                if (!std::is_same<T, __half>::value) {
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) {
+                        const uint32_t top = magnitude(q[i]);
+                        const unsigned big = __ballot_sync(0xFFFFFFFFu, top >= (127u + 15u) << 7), some = __ballot_sync(0xFFFFFFFFu, top >= (127u - 6u) << 7);
+                        bool rows_fit = big == 0;
+#pragma unroll
+                        for (int k = 0; k < kAt; ++k) rows_fit = rows_fit && (some >> k * kRowLanes & kRowMask || low + i * kAt + k >= rows);
+                        fits = fits && rows_fit;
                     }
                 }
+                if (fits) {
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int at_row = low + i * kAt + lane / kRowLanes;
-                    uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                    if (!std::is_same<T, __half>::value) {
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7FFFu, w[k] >> 16 & 0x7FFFu));
+                    for (int i = 0; i < kLoads; ++i) keep(i, q[i], 1.f);
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < kLoads; ++i) {
+                        const uint4 y = fetch(i);
+                        uint32_t top = magnitude(y);
 #pragma unroll
                         for (int o = kRowLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
                         const int e = min(max((int)(top >> 7) - 127, -112), 120) - 8;
                         const int own = __shfl_sync(0xFFFFFFFFu, e, lane % kAt * kRowLanes);       // this thread's row, if it is among these
                         if (lane / kAt == i) qf = a.scale * power_of_two(own);
-                        const float f = power_of_two(-e);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float2 y = to_float2<T>(w[k]);
-                            w[k] = from_float2<__half>(y.x * f, y.y * f);
-                        }
+                        keep(i, y, power_of_two(-e));
                     }
-                    if (!single || X == 0)
-                        *reinterpret_cast<uint4*>(smem + L::kQ + X * L::kOperand + (sub >> 3) * (128 * 128) + at_row * 128 + (((sub & 7) ^ (at_row & 7)) << 4)) =
-                            make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
             proxy_fence();
@@ -454,11 +475,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     const bool edge = side && (kt + 1) * kTileKeys > r.len;        // NaN codes of the step's own values, and what lies behind them
                     uint32_t seen = 0;
                     wait(raw_full + st, raw_phase);
+                    uint4 codes[kIter];                      // all of them, so that the next tile's may come in
+#pragma unroll
+                    for (int i = 0; i < kIter; ++i) codes[i] = *reinterpret_cast<const uint4*>(from + i * 2048);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bars + raw_free + st);
                     wait(free_ + stage, phase ^ 1);
-#pragma unroll 2
+#pragma unroll
                     for (int i = 0; i < kIter; ++i) {
                         const int row = i * kAtOnce + key;
-                        uint4 x = *reinterpret_cast<const uint4*>(from + i * 2048);
+                        uint4 x = codes[i];
                         if (edge) {
                             const int s = kt * kTileKeys + row;
                             if (s >= end) x = make_uint4(0, 0, 0, 0);
@@ -480,10 +506,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     if (seen) atomicOr(nans + (run & (kTileSlots - 1)), 1);
                     proxy_fence();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bars + raw_free + st);
-                        mbar_arrive(bars + full + stage);
-                    }
+                    if (lane == 0) mbar_arrive(bars + full + stage);
                 }
             }
             ++run;
