@@ -196,19 +196,22 @@ int opt_tree_kv_append(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
     a.cos_sin = turn->cos_sin; a.positions = turn->positions; a.rot_dim = turn->rot_dim; a.interleaved = turn->interleaved ? 1 : 0;
     a.q_norm = static_cast<const uint16_t*>(turn->q_norm); a.k_norm = static_cast<const uint16_t*>(turn->k_norm);
     a.eps = turn->eps;
+    a.wide_cs = (reinterpret_cast<uintptr_t>(turn->cos_sin) & 15u) == 0;
     a.wide_w = ((reinterpret_cast<uintptr_t>(turn->q_norm) | reinterpret_cast<uintptr_t>(turn->k_norm)) & 15u) == 0;
     a.page_slots = (step->T + kv->cfg.page - 2) / kv->cfg.page + 1;
     a.page_blocks = step->B * a.page_slots * kv->cfg.kv_heads * 2;
     a.by_heads = ot::FixedDiv::by((unsigned)kv->cfg.kv_heads); a.by_slots = ot::FixedDiv::by((unsigned)a.page_slots);
-    a.by_q_heads = ot::FixedDiv::by((unsigned)kv->cfg.q_heads); a.by_T = ot::FixedDiv::by((unsigned)step->T);
+    a.by_T = ot::FixedDiv::by((unsigned)step->T);
     a.status = kv->status;
     int threads = 0;
     const bool bf16 = kv->cfg.dtype == OPT_TREE_BF16;
     const AppendKernel kernel = D == 64 ? (bf16 ? append_variant<64, __nv_bfloat16>(kv->cfg.page, &threads) : append_variant<64, __half>(kv->cfg.page, &threads))
                                         : (bf16 ? append_variant<128, __nv_bfloat16>(kv->cfg.page, &threads) : append_variant<128, __half>(kv->cfg.page, &threads));
-    const long long rows = q ? (long long)step->B * step->T * kv->cfg.q_heads : 0;
-    const long long per_block = (long long)(threads / 32) * (256 / D) * ot::kAppendQueryRows;
-    const long long blocks = a.page_blocks + (rows + per_block - 1) / per_block;
+    const int per_warp = ot::kAppendRows * (256 / D);
+    a.query_parts = (kv->cfg.q_heads + per_warp - 1) / per_warp;
+    a.by_parts = ot::FixedDiv::by((unsigned)a.query_parts);
+    const long long warps = q ? (long long)step->B * step->T * a.query_parts : 0, per_block = threads / 32;
+    const long long blocks = a.page_blocks + (warps + per_block - 1) / per_block;
     launch_after(kernel, dim3((unsigned)blocks), dim3(threads), 0, static_cast<cudaStream_t>(stream), a);
     kv->launches++;
     return check_launch();

@@ -25,67 +25,88 @@ struct KvAppend {
     int positions, rot_dim, interleaved;
     const uint16_t *q_norm, *k_norm;
     float eps;
-    int wide_q, wide_k, wide_v, wide_out, wide_w;   // rows on 16-byte boundaries
+    int wide_q, wide_k, wide_v, wide_out, wide_w, wide_cs;   // rows on 16-byte boundaries
     int page_slots;                      // most pages a sequence's step can touch
     int page_blocks;                     // CTAs that take pages; the others take queries
-    FixedDiv by_heads, by_slots, by_q_heads, by_T;
+    int query_parts;                     // warps that share a token's query heads
+    FixedDiv by_heads, by_slots, by_parts, by_T;
     int* status;
 };
 
-constexpr int kAppendQueryRows = 4;      // row groups a warp of a query CTA has in flight
+constexpr int kAppendRows = 8;           // row groups a warp of a query CTA takes, all of one token: positions and angles are looked up once
 
 template <class T> __device__ __forceinline__ T rsqrt_of(T x);
 template <> __device__ __forceinline__ float rsqrt_of<float>(float x) { return rsqrtf(x); }
 template <> __device__ __forceinline__ double rsqrt_of<double>(double x) { return 1.0 / sqrt(x); }
 
-// Norm and rotation of one row: a lane holds eight consecutive elements, D/8 consecutive lanes a row.  F: float, or double where
-// the largest value lies so near a border of the scale that single precision could take the other side.
-template <int D, class T, class F>
-__device__ __forceinline__ void turn_row(const KvAppend& a, const uint16_t* w, int pos, const float (&in)[8], F (&x)[8]) {
-    constexpr int kLanes = D / 8;
-    const int sub = threadIdx.x & (kLanes - 1);
+// A lane holds eight consecutive elements of a row, D / 8 consecutive lanes a row.  Rotation is x' = x c + y s with y the other element of
+// the pair, which another lane (`partner`) or this one holds, and the sign in s; elements that are not rotated have c = 1, s = 0.
+struct KvAngles {
+    float c[8], s[8];
+};
+__device__ __forceinline__ int kv_partner(const KvAppend& a, int sub) {
+    const int half = a.rot_dim >> 4;                         // in lanes
+    return a.interleaved || sub >= 2 * half ? sub : (sub < half ? sub + half : sub - half);
+}
+__device__ __forceinline__ void load4(const float* p, int wide, float* x) {
+    if (wide) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (F)in[i];
-    if (w) {
+        for (int i = 0; i < 4; ++i) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ void kv_angles(const KvAppend& a, int sub, int pos, KvAngles& g) {
+    const int half = a.rot_dim >> 1, at = sub * 8;
+    const float* cs = a.cos_sin + (long long)pos * a.rot_dim;
+    if (at >= a.rot_dim) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { g.c[i] = 1.f; g.s[i] = 0.f; }
+    } else if (a.interleaved) {
+        float c[4], s[4];
+        load4(cs + at / 2, a.wide_cs, c);
+        load4(cs + half + at / 2, a.wide_cs, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { g.c[2 * i] = g.c[2 * i + 1] = c[i]; g.s[2 * i] = -s[i]; g.s[2 * i + 1] = s[i]; }
+    } else {
+        const float* from = cs + (at < half ? at : at - half);
+        load4(from, a.wide_cs, g.c); load4(from + 4, a.wide_cs, g.c + 4);
+        load4(from + half, a.wide_cs, g.s); load4(from + half + 4, a.wide_cs, g.s + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g.s[i] = at < half ? -g.s[i] : g.s[i];
+    }
+}
+// Norm and rotation of one row.  w: the weights of this lane's elements.  F: float, or double where the largest value lies so near a
+// border of the scale that single precision could take the other side.
+template <int D, class F>
+__device__ __forceinline__ void turn_row(const KvAppend& a, bool norm, const float (&w)[8], const KvAngles& g, int partner, F (&x)[8]) {
+    constexpr int kLanes = D / 8;
+    if (norm) {
         F sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         const F r = rsqrt_of<F>(sum / (F)D + (F)a.eps);
-        float wf[8];
-        unpack8<T>(load8(w + sub * 8, a.wide_w), wf);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (F)wf[i];
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (F)w[i];
     }
     if (a.rot_dim == 0) return;
-    const float* cs = a.cos_sin + (long long)pos * a.rot_dim;
-    const int half = a.rot_dim >> 1, at = sub * 8;
     if (a.interleaved) {
-        if (at >= a.rot_dim) return;
-        float c[4], s[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { c[i] = cs[at / 2 + i]; s[i] = cs[half + at / 2 + i]; }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const F p = x[2 * i], q = x[2 * i + 1];
-            x[2 * i] = p * (F)c[i] - q * (F)s[i];
-            x[2 * i + 1] = q * (F)c[i] + p * (F)s[i];
+        for (int i = 0; i < 8; i += 2) {
+            const F p = x[i], q = x[i + 1];
+            x[i] = p * (F)g.c[i] + q * (F)g.s[i];
+            x[i + 1] = q * (F)g.c[i + 1] + p * (F)g.s[i + 1];
         }
     } else {
-        const bool low = at < half;
-        const int partner = at >= a.rot_dim ? sub : (low ? sub + half / 8 : sub - half / 8);
         const int lane = (threadIdx.x & 31 & ~(kLanes - 1)) + partner;
-        F other[8];
+        F y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) other[i] = __shfl_sync(0xFFFFFFFFu, x[i], lane);
-        if (at >= a.rot_dim) return;
-        const float* c = cs + (low ? at : at - half);
+        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xFFFFFFFFu, x[i], lane);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const F cc = (F)c[i], ss = (F)c[half + i];
-            x[i] = low ? x[i] * cc - other[i] * ss : x[i] * cc + other[i] * ss;
-        }
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * (F)g.c[i] + y[i] * (F)g.s[i];
     }
 }
 
@@ -100,40 +121,39 @@ __device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int 
     return pos;
 }
 
-// The queries: rows (sequence, token, head) in that order.
+// The queries: a warp takes kAppendRows groups of heads of one token.
 template <int D, class T>
-__device__ __forceinline__ void append_queries(const KvAppend& a, int block) {
+__device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
     const int lane = threadIdx.x & 31, sub = lane & (kLanes - 1);
-    const unsigned rows = (unsigned)a.step.B * a.step.T * a.shape.q_heads;
-    const long long first = ((long long)block * (blockDim.x >> 5) + (threadIdx.x >> 5)) * (kRows * kAppendQueryRows) + lane / kLanes;
-    uint4 raw[kAppendQueryRows];
-    int pos[kAppendQueryRows];
-    long long to[kAppendQueryRows];
+    const unsigned item = block * (blockDim.x >> 5) + (threadIdx.x >> 5), bt = a.by_parts.div(item), part = item - bt * a.query_parts;
+    const unsigned b = a.by_T.div(bt);
+    const int j = (int)(bt - b * a.step.T), h0 = (int)part * kAppendRows * kRows + lane / kLanes;
+    if (b >= (unsigned)a.step.B) return;
+    int len, tokens;
+    if (!kv_sequence(a.shape, a.step, b, len, tokens, a.status) || j >= tokens) return;
+    const uint16_t* from = a.q.data + b * a.q.batch + j * a.q.token + sub * 8;
+    uint16_t* to = const_cast<uint16_t*>(a.q_out.data) + b * a.q_out.batch + j * a.q_out.token + sub * 8;
+    uint4 raw[kAppendRows];
 #pragma unroll
-    for (int i = 0; i < kAppendQueryRows; ++i) {
-        const long long r = first + i * kRows;
-        to[i] = -1; pos[i] = 0;
+    for (int i = 0; i < kAppendRows; ++i) {
         raw[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows) {
-            const unsigned bt = a.by_q_heads.div((unsigned)r), h = (unsigned)r - bt * a.shape.q_heads;
-            const unsigned b = a.by_T.div(bt), j = bt - b * a.step.T;
-            int len, tokens;
-            if (kv_sequence(a.shape, a.step, b, len, tokens, a.status) && (int)j < tokens) {
-                raw[i] = load8(a.q.data + b * a.q.batch + j * a.q.token + h * a.q.head + sub * 8, a.wide_q);
-                to[i] = b * a.q_out.batch + j * a.q_out.token + h * a.q_out.head + sub * 8;
-                pos[i] = kv_position(a, b, j, len);
-            }
-        }
+        if (h0 + i * kRows < a.shape.q_heads) raw[i] = load8(from + (h0 + i * kRows) * a.q.head, a.wide_q);
     }
+    float w[8] = {};
+    KvAngles g;
+    if (a.q_norm) unpack8<T>(load8(a.q_norm + sub * 8, a.wide_w), w);
+    if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, j, len), g);
+    const int partner = kv_partner(a, sub);
 #pragma unroll
-    for (int i = 0; i < kAppendQueryRows; ++i) {
-        float in[8], x[8];
-        unpack8<T>(raw[i], in);
-        turn_row<D, T, float>(a, a.q_norm, pos[i], in, x);
-        if (to[i] >= 0) {
+    for (int i = 0; i < kAppendRows; ++i) {
+        if (part * kAppendRows * kRows + i * kRows >= (unsigned)a.shape.q_heads) break;    // the same for the whole warp
+        float x[8];
+        unpack8<T>(raw[i], x);
+        turn_row<D, float>(a, a.q_norm != nullptr, w, g, partner, x);
+        if (h0 + i * kRows < a.shape.q_heads) {
             const uint4 o = make_uint4(from_float2<T>(x[0], x[1]), from_float2<T>(x[2], x[3]), from_float2<T>(x[4], x[5]), from_float2<T>(x[6], x[7]));
-            store8(const_cast<uint16_t*>(a.q_out.data) + to[i], o, a.wide_out);
+            store8(to + (h0 + i * kRows) * a.q_out.head, o, a.wide_out);
         }
     }
 }
@@ -152,7 +172,7 @@ template <int D, class T, int kThreadsN, int kPasses>
 __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_constant__ KvAppend a) {
     grid_dependency_wait();
     if ((int)blockIdx.x >= a.page_blocks) {
-        append_queries<D, T>(a, blockIdx.x - a.page_blocks);
+        append_queries<D, T>(a, blockIdx.x - (unsigned)a.page_blocks);
         return;
     }
     constexpr int kLanes = D / 8, kRows = 32 / kLanes, kWarpsN = kThreadsN / 32;
@@ -169,6 +189,17 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
     const int start = at << a.shape.page_shift;                              // first slot of the page
     const int lo = max(len, start), hi = min(len + tokens, start + page);    // the step's slots in it
     if (lo >= hi) return;
+    const KvRows& src = values ? a.v : a.k;
+    const uint16_t* from = src.data + b * src.batch + h * src.head + sub * 8;
+    const bool wide = values ? a.wide_v : a.wide_k;
+    const int n = hi - lo;
+    uint4 raw[kPasses];                                                      // on their way while the page is looked up
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (r < n) raw[i] = load8(from + (long long)(lo - len + r) * src.token, wide);
+    }
     const int id = kv_page(a.shape, a.table, b, at, a.status);
     if (id < 0) return;
     const long long head = (long long)id * a.shape.kv_heads + h;
@@ -176,56 +207,50 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
     float* scale = (values ? a.vs : a.ks) + head;
     const bool older = lo > start;
     const float was = older ? *scale : 0.f;
-    const KvRows& src = values ? a.v : a.k;
-    const uint16_t* from = src.data + b * src.batch + h * src.head + sub * 8;
-    const bool wide = values ? a.wide_v : a.wide_k;
+    const bool turns = !values && (a.k_norm || a.rot_dim);
+    const int partner = kv_partner(a, sub);
+    float w[8] = {};
+    if (turns && a.k_norm) unpack8<T>(load8(a.k_norm + sub * 8, a.wide_w), w);
 
     float x[kPasses][8];
     float most = 0.f;
-    const int n = hi - lo;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-        const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (r < n) raw = load8(from + (long long)(lo - len + r) * src.token, wide);
-        unpack8<T>(raw, x[i]);
-    }
-    if (!values) {
-#pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            if ((i * kWarpsN + warp) * kRows >= n) break;                    // the same for the whole warp
+        unpack8<T>(raw[i], x[i]);
+        if (turns && (i * kWarpsN + warp) * kRows < n) {                     // the same for the whole warp
             const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
-            const int pos = r < n ? kv_position(a, b, lo - len + r, len) : 0;
-            float in[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) in[e] = x[i][e];
-            turn_row<D, T, float>(a, a.k_norm, pos, in, x[i]);
+            KvAngles g;
+            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len), g);
+            turn_row<D, float>(a, a.k_norm != nullptr, w, g, partner, x[i]);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_abs(x[i][e]));
+    }
     most = warp_max_f32(most);
     if (lane == 0) warp_max[warp] = __float_as_uint(most);
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWarpsN; ++w) most = fmaxf(most, __uint_as_float(warp_max[w]));
+    for (int w1 = 0; w1 < kWarpsN; ++w1) most = fmaxf(most, __uint_as_float(warp_max[w1]));
     // Single precision is off by less than 1e-6; nearer than 1e-5 to a border the largest value is found again in double
     // precision, so that the scale, which is a whole power of two, does not hang on a rounding.
     const uint32_t frac = __float_as_uint(most) & 0x7FFFFFu;
     int e = scale_exponent(__float_as_uint(most));
-    if (!values && (a.k_norm || a.rot_dim) && frac > 0x600000u - 147u && frac < 0x600000u + 147u) {
+    if (turns && frac > 0x600000u - 147u && frac < 0x600000u + 147u) {
         double exact = 0.0;
+#pragma unroll 1
         for (int i = 0; i < kPasses; ++i) {
             if ((i * kWarpsN + warp) * kRows >= n) break;
             const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
-            uint4 raw = make_uint4(0, 0, 0, 0);
-            if (r < n) raw = load8(from + (long long)(lo - len + r) * src.token, wide);
+            uint4 again = make_uint4(0, 0, 0, 0);
+            if (r < n) again = load8(from + (long long)(lo - len + r) * src.token, wide);
             float in[8];
             double y[8];
-            unpack8<T>(raw, in);
-            turn_row<D, T, double>(a, a.k_norm, r < n ? kv_position(a, b, lo - len + r, len) : 0, in, y);
+            unpack8<T>(again, in);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c] = in[c];
+            KvAngles g;
+            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len), g);
+            turn_row<D, double>(a, a.k_norm != nullptr, w, g, partner, y);
 #pragma unroll
             for (int c = 0; c < 8; ++c) exact = fmax(exact, finite_abs(y[c]));
         }
@@ -233,7 +258,7 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
         if (lane == 0) warp_max64[warp] = bits;
         __syncthreads();
         unsigned long long all = 0;
-        for (int w = 0; w < kWarpsN; ++w) all = warp_max64[w] > all ? warp_max64[w] : all;
+        for (int w1 = 0; w1 < kWarpsN; ++w1) all = warp_max64[w1] > all ? warp_max64[w1] : all;
         // 1.75 in the fraction of a double
         e = (int)(all >> 52) - 1023 - 8 + ((all & 0xFFFFFFFFFFFFFull) > 0xC000000000000ull ? 1 : 0);
         e = e < kLeastScaleExp ? kLeastScaleExp : e;
