@@ -273,7 +273,7 @@ int opt_tree_step_host(opt_tree_ctx *ctx, const void *draft_logits_bf16, const v
  *                                        tokens before it (T = 1: plain decoding; a prompt's chunk)
  *   rows     q, k, v and outputs: 16-bit elements (dtype of the handle) [B][T][heads][head_dim], strides in elements, head_dim
  *            contiguous; any base a 16-bit element may have, fastest where base and strides are multiples of 16 bytes.
- * Tokens beyond a sequence's nodes + 1 are padding: neither read nor written anywhere.
+ * Tokens beyond a sequence's nodes + 1 are padding: their rows are not used and not written anywhere.
  *
  * A handle owns a workspace and a status word only and belongs to the device that was current at its creation; calls are made
  * with that device current (otherwise OPT_TREE_ERR_INVALID_ARG).  The calls only enqueue work on `stream`, may be captured into

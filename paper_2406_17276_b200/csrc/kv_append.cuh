@@ -35,10 +35,6 @@ struct KvAppend {
 
 constexpr int kAppendRows = 8;           // row groups a warp of a query CTA takes, all of one token: positions and angles are looked up once
 
-template <class T> __device__ __forceinline__ T rsqrt_of(T x);
-template <> __device__ __forceinline__ float rsqrt_of<float>(float x) { return rsqrtf(x); }
-template <> __device__ __forceinline__ double rsqrt_of<double>(double x) { return 1.0 / sqrt(x); }
-
 // A lane holds eight consecutive elements of a row, D / 8 consecutive lanes a row.  Rotation is x' = x c + y s with y the other element of
 // the pair, which another lane (`partner`) or this one holds, and the sign in s; elements that are not rotated have c = 1, s = 0.
 struct KvAngles {
@@ -77,42 +73,98 @@ __device__ __forceinline__ void kv_angles(const KvAppend& a, int sub, int pos, K
         for (int i = 0; i < 8; ++i) g.s[i] = at < half ? -g.s[i] : g.s[i];
     }
 }
-// Norm and rotation of one row.  w: the weights of this lane's elements.  F: float, or double where the largest value lies so near a
-// border of the scale that single precision could take the other side.
-template <int D, class F>
-__device__ __forceinline__ void turn_row(const KvAppend& a, bool norm, const float (&w)[8], const KvAngles& g, int partner, F (&x)[8]) {
+// Norm and rotation with what does not depend on the row folded together, in packed pairs: x' = r (x (w c) + y (w_y s)), r the norm's factor.
+struct KvFold {
+    unsigned long long c[4], s[4];
+};
+template <class T>
+__device__ __forceinline__ void kv_fold(const KvAppend& a, const uint16_t* weights, const KvAngles& g, int sub, int partner, KvFold& f) {
+    float c[8], s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { c[i] = a.rot_dim ? g.c[i] : 1.f; s[i] = a.rot_dim ? g.s[i] : 0.f; }
+    if (weights) {
+        float w[8], y[8];
+        unpack8<T>(load8(weights + sub * 8, a.wide_w), w);
+        unpack8<T>(load8(weights + partner * 8, a.wide_w), y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] *= w[i]; s[i] *= a.interleaved ? y[i ^ 1] : y[i]; }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f.c[i] = pack2(c[2 * i], c[2 * i + 1]); f.s[i] = pack2(s[2 * i], s[2 * i + 1]); }
+}
+template <int D, class T>
+__device__ __forceinline__ void turn_fast(const KvAppend& a, bool norm, const KvFold& f, int partner, uint4 raw, float (&out)[8]) {
     constexpr int kLanes = D / 8;
+    unsigned long long x[4];
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 v = to_float2<T>(w[i]); x[i] = pack2(v.x, v.y); }
+    float r = 1.f;
     if (norm) {
-        F sum = 0;
+        unsigned long long s2 = mul2(x[0], x[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) s2 = fma2(x[i], x[i], s2);
+        float lo, hi;
+        unpack2(s2, lo, hi);
+        float sum = lo + hi;
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        r = rsqrtf(sum * (1.f / D) + a.eps);
+    }
+    const int lane = (threadIdx.x & 31 & ~(kLanes - 1)) + partner;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned long long z = mul2(x[i], f.c[i]);
+        if (a.rot_dim) {
+            unsigned long long y;
+            if (a.interleaved) {
+                float lo, hi;
+                unpack2(x[i], lo, hi);
+                y = pack2(hi, lo);
+            } else {
+                const float2 v = to_float2<T>(__shfl_sync(0xFFFFFFFFu, w[i], lane));
+                y = pack2(v.x, v.y);
+            }
+            z = fma2(y, f.s[i], z);
+        }
+        if (norm) z = mul2(z, pack2(r, r));
+        unpack2(z, out[2 * i], out[2 * i + 1]);
+    }
+}
+// The same of one row in double precision, for where the largest value lies so near a border of the scale that single precision could
+// take the other side.
+template <int D, class T>
+__device__ __forceinline__ void turn_exact(const KvAppend& a, const uint16_t* weights, const KvAngles& g, int sub, int partner, uint4 raw, double (&x)[8]) {
+    constexpr int kLanes = D / 8;
+    float in[8];
+    unpack8<T>(raw, in);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = in[i];
+    if (weights) {
+        double sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        const F r = rsqrt_of<F>(sum / (F)D + (F)a.eps);
+        const double r = 1.0 / sqrt(sum / D + (double)a.eps);
+        unpack8<T>(load8(weights + sub * 8, a.wide_w), in);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (F)w[i];
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * in[i];
     }
     if (a.rot_dim == 0) return;
-    if (a.interleaved) {
+    const int lane = (threadIdx.x & 31 & ~(kLanes - 1)) + partner;
+    double y[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const F p = x[i], q = x[i + 1];
-            x[i] = p * (F)g.c[i] + q * (F)g.s[i];
-            x[i + 1] = q * (F)g.c[i + 1] + p * (F)g.s[i + 1];
-        }
-    } else {
-        const int lane = (threadIdx.x & 31 & ~(kLanes - 1)) + partner;
-        F y[8];
+    for (int i = 0; i < 8; ++i) y[i] = a.interleaved ? x[i ^ 1] : __shfl_sync(0xFFFFFFFFu, x[i], lane);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xFFFFFFFFu, x[i], lane);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * (F)g.c[i] + y[i] * (F)g.s[i];
-    }
+    for (int i = 0; i < 8; ++i) x[i] = x[i] * g.c[i] + y[i] * g.s[i];
 }
 
-__device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int len) {
+// base: the sequence's base_pos, loaded by the caller together with its lengths (kv_base).
+__device__ __forceinline__ int kv_base(const KvAppend& a, int b) { return a.rot_dim && a.step.base_pos ? a.step.base_pos[b] : 0; }
+__device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int len, int base) {
     if (a.rot_dim == 0) return 0;
-    const int base = a.step.base_pos ? a.step.base_pos[b] : len;
+    if (!a.step.base_pos) base = len;
     const int pos = j == 0 || !a.step.position_ids ? base + j : a.step.position_ids[(long long)b * (a.step.T - 1) + j - 1];
     if ((unsigned)pos >= (unsigned)a.positions) {
         set_status(a.status, kErrInternal);
@@ -130,8 +182,7 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
     const unsigned b = a.by_T.div(bt);
     const int j = (int)(bt - b * a.step.T), h0 = (int)part * kAppendRows * kRows + lane / kLanes;
     if (b >= (unsigned)a.step.B) return;
-    int len, tokens;
-    if (!kv_sequence(a.shape, a.step, b, len, tokens, a.status) || j >= tokens) return;
+    // what is certain to be needed is on its way before the lengths are known (rows of padding may be read, but are not used)
     const uint16_t* from = a.q.data + b * a.q.batch + j * a.q.token + sub * 8;
     uint16_t* to = const_cast<uint16_t*>(a.q_out.data) + b * a.q_out.batch + j * a.q_out.token + sub * 8;
     uint4 raw[kAppendRows];
@@ -140,17 +191,19 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
         raw[i] = make_uint4(0, 0, 0, 0);
         if (h0 + i * kRows < a.shape.q_heads) raw[i] = load8(from + (h0 + i * kRows) * a.q.head, a.wide_q);
     }
-    float w[8] = {};
+    const int base = kv_base(a, b);
+    int len, tokens;
+    if (!kv_sequence(a.shape, a.step, b, len, tokens, a.status) || j >= tokens) return;
     KvAngles g;
-    if (a.q_norm) unpack8<T>(load8(a.q_norm + sub * 8, a.wide_w), w);
-    if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, j, len), g);
+    KvFold f;
     const int partner = kv_partner(a, sub);
+    if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, j, len, base), g);
+    kv_fold<T>(a, a.q_norm, g, sub, partner, f);
 #pragma unroll
     for (int i = 0; i < kAppendRows; ++i) {
         if (part * kAppendRows * kRows + i * kRows >= (unsigned)a.shape.q_heads) break;    // the same for the whole warp
         float x[8];
-        unpack8<T>(raw[i], x);
-        turn_row<D, float>(a, a.q_norm != nullptr, w, g, partner, x);
+        turn_fast<D, T>(a, a.q_norm != nullptr, f, partner, raw[i], x);
         if (h0 + i * kRows < a.shape.q_heads) {
             const uint4 o = make_uint4(from_float2<T>(x[0], x[1]), from_float2<T>(x[2], x[3]), from_float2<T>(x[4], x[5]), from_float2<T>(x[6], x[7]));
             store8(to + (h0 + i * kRows) * a.q_out.head, o, a.wide_out);
@@ -169,7 +222,7 @@ __device__ __forceinline__ double finite_abs(double x) {
 
 // kPasses: row groups per warp that cover a page.
 template <int D, class T, int kThreadsN, int kPasses>
-__global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_constant__ KvAppend a) {
+__global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN == 128 ? 6 : 3) kv_append_kernel(const __grid_constant__ KvAppend a) {
     grid_dependency_wait();
     if ((int)blockIdx.x >= a.page_blocks) {
         append_queries<D, T>(a, blockIdx.x - (unsigned)a.page_blocks);
@@ -183,6 +236,7 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
     const bool values = blockIdx.x & 1;
     const unsigned bp = a.by_heads.div(item), h = item - bp * a.shape.kv_heads;
     const unsigned b = a.by_slots.div(bp), slot = bp - b * a.page_slots;
+    const int base = values ? 0 : kv_base(a, b);
     int len, tokens;
     if (!kv_sequence(a.shape, a.step, b, len, tokens, a.status)) return;
     const int page = a.shape.page, at = (len >> a.shape.page_shift) + slot;
@@ -209,19 +263,20 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
     const float was = older ? *scale : 0.f;
     const bool turns = !values && (a.k_norm || a.rot_dim);
     const int partner = kv_partner(a, sub);
-    float w[8] = {};
-    if (turns && a.k_norm) unpack8<T>(load8(a.k_norm + sub * 8, a.wide_w), w);
 
     float x[kPasses][8];
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-        unpack8<T>(raw[i], x[i]);
         if (turns && (i * kWarpsN + warp) * kRows < n) {                     // the same for the whole warp
             const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
             KvAngles g;
-            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len), g);
-            turn_row<D, float>(a, a.k_norm != nullptr, w, g, partner, x[i]);
+            KvFold f;
+            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len, base), g);
+            kv_fold<T>(a, a.k_norm, g, sub, partner, f);
+            turn_fast<D, T>(a, a.k_norm != nullptr, f, partner, raw[i], x[i]);
+        } else {
+            unpack8<T>(raw[i], x[i]);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_abs(x[i][e]));
@@ -243,14 +298,10 @@ __global__ void __launch_bounds__(kThreadsN) kv_append_kernel(const __grid_const
             const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
             uint4 again = make_uint4(0, 0, 0, 0);
             if (r < n) again = load8(from + (long long)(lo - len + r) * src.token, wide);
-            float in[8];
             double y[8];
-            unpack8<T>(again, in);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) y[c] = in[c];
             KvAngles g;
-            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len), g);
-            turn_row<D, double>(a, a.k_norm != nullptr, w, g, partner, y);
+            if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len, base), g);
+            turn_exact<D, T>(a, a.k_norm, g, sub, partner, again, y);
 #pragma unroll
             for (int c = 0; c < 8; ++c) exact = fmax(exact, finite_abs(y[c]));
         }
