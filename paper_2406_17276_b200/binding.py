@@ -456,12 +456,12 @@ class TreeKV:
 
     def _call(self, name: str, *args):
         """Calls with the handle's device current and its current stream as the last argument."""
-        f = getattr(lib(), name)
-        if _current_device() == self._at:
-            code = f(self._kv, *args, _current_stream(self._at))
+        at = self._at
+        if _current_device() == at:
+            code = getattr(_lib, name)(self._kv, *args, _current_stream(at))
         else:
             with torch.cuda.device(self.device):
-                code = f(self._kv, *args, _current_stream(self._at))
+                code = getattr(_lib, name)(self._kv, *args, _current_stream(at))
         if code != OK:
             raise OptTreeError(code, name)
 

@@ -75,7 +75,8 @@ using AttendKernel = void (*)(ot::KvAttend);
 using JoinKernel = void (*)(ot::KvAttend);
 struct AttendVariant { AttendKernel kernel; size_t smem; int per_sm, threads, rows, keys; JoinKernel join; };
 template <int D, int NT, class T> AttendVariant few_variant() {
-    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)ot::FewLayout<D, NT>::kBytes, NT == 1 ? 2 : 1, ot::kFewThreads, 8 * NT, ot::kFewKeys, nullptr};
+    using L = ot::FewLayout<D, NT>;
+    return AttendVariant{ot::kv_attend_few_kernel<D, NT, T>, (size_t)L::kBytes, L::kPerSm, L::kThreads, L::kRows, L::kKeys, nullptr};
 }
 template <int D, class T> AttendVariant attend_variant(int rows) {
     if (rows <= 8) return few_variant<D, 1, T>();
@@ -90,10 +91,10 @@ AttendVariant attend_for(const opt_tree_kv_config& c, int rows) {
     return bf16 ? attend_variant<128, __nv_bfloat16>(rows) : attend_variant<128, __half>(rows);
 }
 const int kVariantRows[] = {1, 16, 17};  // one row count for each variant
-constexpr size_t kMaxParts = 2;          // CTAs per SM at most, and row tiles of a CTA
+constexpr size_t kMaxTiles = 2;          // CTAs of an SM, and row tiles of a CTA, at most
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
-// Bytes of the two parts that each CTA may leave of a cut row tile, per SM: two CTAs with 16 rows each, or one with two tiles of 128.
+// Bytes of the two parts that each CTA may leave of cut row tiles, per SM: two CTAs with 16 rows each, or one with two tiles of 128.
 template <int D> size_t part_bytes(long long rows) {
     const size_t few = (size_t)2 * 2 * ot::kv_part_floats<16, D>() * sizeof(float), tiles = (size_t)2 * 2 * ot::kv_part_floats<ot::kTileRows, D>() * sizeof(float);
     return rows <= 16 ? few : tiles;
@@ -114,7 +115,7 @@ size_t opt_tree_kv_workspace_bytes(const opt_tree_kv_config* cfg) {
         cudaGetLastError();
         sms = 148;                                   // no device here: the size on a B200
     }
-    return 256 + align256(sms * kMaxParts * sizeof(int)) + align256(sms * sizeof(ot::KvRun)) + sms * parts_per_sm(*cfg);
+    return 256 + align256(sms * kMaxTiles * sizeof(int)) + align256(sms * sizeof(ot::KvRun)) + sms * parts_per_sm(*cfg);
 }
 
 int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
@@ -154,7 +155,7 @@ int opt_tree_kv_create(opt_tree_kv** out, const opt_tree_kv_config* cfg) {
     char* at = static_cast<char*>(kv->base);
     kv->status = reinterpret_cast<int*>(at);
     kv->arrived = reinterpret_cast<int*>(at + 256);
-    at += 256 + align256(kv->sms * kMaxParts * sizeof(int));
+    at += 256 + align256(kv->sms * kMaxTiles * sizeof(int));
     kv->cuts = reinterpret_cast<ot::KvRun*>(at);
     kv->parts = reinterpret_cast<float*>(at + align256(kv->sms * sizeof(ot::KvRun)));
     *out = kv;

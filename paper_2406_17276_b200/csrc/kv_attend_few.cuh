@@ -16,8 +16,6 @@
 
 namespace ot {
 
-constexpr int kFewWarps = 8, kFewThreads = kFewWarps * 32, kFewKeys = kFewWarps * 16;
-
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -27,22 +25,24 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
 // page's scale over the largest so far, so that pages with scales down to 2^-24 of the largest keep that accuracy.
 constexpr float kProbUnit = 4096.f;
 
-// NT: row groups of eight.
+// NT: row groups of eight.  Two CTAs an SM where registers allow (one of 16 warps: 13.8 us against 12.5 for one token over 1500, 175 against
+// 170 for 32 over 16384).
 template <int D, int NT> struct FewLayout {
-    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kWarps = 8, kThreads = kWarps * 32, kKeys = kWarps * 16, kPerSm = NT == 1 ? 2 : 1;
+    static constexpr int kStages = (D == 128 ? 6 : 12) / kPerSm;
     static constexpr int kKBytes = 16 * D, kVGroup = 4 * D + 32, kStage = kKBytes + 4 * kVGroup;
     static constexpr int kRows = 8 * NT;
-    static constexpr int kRing = kFewWarps * kStages * kStage;
-    static constexpr int kMerge = kFewWarps * (kRows * D + 2 * kRows) * 4;   // the warps' parts, over the ring
+    static constexpr int kRing = kWarps * kStages * kStage;
+    static constexpr int kMerge = kWarps * (kRows * D + 2 * kRows) * 4;   // the warps' parts, over the ring
     static constexpr int kBig = kRing > kMerge ? kRing : kMerge;
-    static constexpr int kBars = kBig, kWord = kBars + kFewWarps * kStages * 8;
+    static constexpr int kBars = kBig, kWord = kBars + kWarps * kStages * 8;
     static constexpr int kBytes = kWord + 16;
 };
 
 template <int D, int NT, class T>
-__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_kernel(const __grid_constant__ KvAttend a) {
+__global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::kPerSm) kv_attend_few_kernel(const __grid_constant__ KvAttend a) {
     using L = FewLayout<D, NT>;
-    constexpr int kRows = L::kRows, kStages = L::kStages, kChunks = D / 64, kSteps = D / 16, kVWords = D / 32;
+    constexpr int kRows = L::kRows, kStages = L::kStages, kKeys = L::kKeys, kChunks = D / 64, kSteps = D / 16, kVWords = D / 32;
     extern __shared__ __align__(128) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     unsigned char* ring = smem + warp * kStages * L::kStage;
@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
     mbar_fence_init();
     __syncwarp();
     grid_dependency_wait();
-    KvWalk<kRows, kFewKeys, false> walk;
+    KvWalk<kRows, kKeys, false> walk;
     if (!walk.begin(a, blockIdx.x, gridDim.x)) return;
     KvRun r;
     uint32_t count = 0;                                      // blocks this warp has consumed: its place in the ring
@@ -61,27 +61,46 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
     while (walk.next(a, r)) {
         const int rows = min(kRows, r.tokens * a.group - r.rt * kRows);
         // this warp's blocks of 16 keys: one a tile
-        const int key0 = (r.k0 * kFewWarps + warp) * 16;
-        const int blocks = key0 < r.keys ? min(r.k1 - r.k0, (r.keys - key0 + kFewKeys - 1) / kFewKeys) : 0;
+        const int key0 = (r.k0 * L::kWarps + warp) * 16;
+        const int blocks = key0 < r.keys ? min(r.k1 - r.k0, (r.keys - key0 + L::kKeys - 1) / L::kKeys) : 0;
+        // queries: rows g and g + 8, elements in the order in which the lanes hold keys.  bf16 rows are brought to half precision by
+        // a power of two of their own (exact but for elements below 2^-22 of the row's largest)
+        uint4 raw[NT][kChunks * 2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int row = n * 8 + g, full = r.rt * kRows + row;
+#pragma unroll
+            for (int i = 0; i < kChunks * 2; ++i) raw[n][i] = make_uint4(0, 0, 0, 0);
+            if (row < rows) {
+                const int token = (int)a.by_group.div((unsigned)full), hq = r.h * a.group + full - token * a.group;
+                const uint16_t* q = a.q.data + r.b * a.q.batch + token * a.q.token + hq * a.q.head;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) raw[n][c * 2 + i] = load8(q + c * 64 + t * 16 + i * 8, a.wide_q);
+            }
+        }
         // pages and scales of 32 blocks at a time, a lane each; the next 32 are fetched while these are in use
         int id[2];
         float ks[2], vs[2];
-        auto look = [&](int chunk, int& i, float& k, float& v) {
+        auto look = [&](int chunk) {
             const int at = chunk * 32 + lane;
-            i = 0; k = v = 0.f;
-            if (at < blocks) {
-                i = max(0, kv_page(a.shape, a.table, r.b, (key0 + at * kFewKeys) >> a.shape.page_shift, a.status));
+            return at < blocks ? max(0, kv_page(a.shape, a.table, r.b, (key0 + at * L::kKeys) >> a.shape.page_shift, a.status)) : -1;
+        };
+        auto scales = [&](int i, float& k, float& v) {
+            k = v = 0.f;
+            if (i >= 0) {
                 const long long head = (long long)i * a.shape.kv_heads + r.h;
                 k = a.ks[head]; v = a.vs[head];
             }
         };
-        look(0, id[0], ks[0], vs[0]);
-        look(1, id[1], ks[1], vs[1]);
+        id[0] = look(0);
+        id[1] = blocks > 32 ? look(1) : -1;
         auto fetch = [&](int i, int page_id) {               // lane 0: block i of this run into its stage
             const uint32_t at = count + i;
             unsigned char* stage = ring + at % kStages * L::kStage;
             unsigned long long* bar = bars + at % kStages;
-            const long long row = ((long long)page_id * a.shape.kv_heads + r.h) * a.shape.page + ((key0 + i * kFewKeys) & (a.shape.page - 1));
+            const long long row = ((long long)page_id * a.shape.kv_heads + r.h) * a.shape.page + ((key0 + i * L::kKeys) & (a.shape.page - 1));
             mbar_expect_tx(bar, 32 * D);
             bulk_load(stage, a.kc + row * D, 16 * D, bar);
 #pragma unroll
@@ -92,30 +111,18 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
             const int p = __shfl_sync(0xFFFFFFFFu, id[0], i);
             if (lane == 0 && i < blocks && !dead) fetch(i, p);
         }
-        // queries: rows g and g + 8, elements in the order in which the lanes hold keys.  bf16 rows are brought to half precision by
-        // a power of two of their own (exact but for elements below 2^-22 of the row's largest)
+        scales(id[0], ks[0], vs[0]);
+        scales(id[1], ks[1], vs[1]);
         uint32_t qa[NT][kSteps][2];
         float qf[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int row = n * 8 + g, full = r.rt * kRows + row;
-            uint4 raw[kChunks * 2];
-#pragma unroll
-            for (int i = 0; i < kChunks * 2; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-            if (row < rows) {
-                const int token = (int)a.by_group.div((unsigned)full), hq = r.h * a.group + full - token * a.group;
-                const uint16_t* q = a.q.data + r.b * a.q.batch + token * a.q.token + hq * a.q.head;
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) raw[c * 2 + i] = load8(q + c * 64 + t * 16 + i * 8, a.wide_q);
-            }
             float f = 1.f, unit = 1.f;
             if (!std::is_same<T, __half>::value) {
                 uint32_t top = 0;                            // largest magnitude, by its bits
 #pragma unroll
                 for (int i = 0; i < kChunks * 2; ++i) {
-                    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                    const uint32_t w[4] = {raw[n][i].x, raw[n][i].y, raw[n][i].z, raw[n][i].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7FFFu, w[e] >> 16 & 0x7FFFu));
                 }
@@ -128,7 +135,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
             qf[n] = unit * a.scale;
 #pragma unroll
             for (int i = 0; i < kChunks * 2; ++i) {
-                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                const uint32_t w[4] = {raw[n][i].x, raw[n][i].y, raw[n][i].z, raw[n][i].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 x = to_float2<T>(w[e]);
@@ -150,7 +157,8 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
         for (int i = 0; i < blocks; ++i) {
             if (i && (i & 31) == 0) {
                 id[0] = id[1]; ks[0] = ks[1]; vs[0] = vs[1];
-                look((i >> 5) + 1, id[1], ks[1], vs[1]);
+                id[1] = look((i >> 5) + 1);
+                scales(id[1], ks[1], vs[1]);
             }
             const float kscale = __shfl_sync(0xFFFFFFFFu, ks[0], i & 31), vscale = __shfl_sync(0xFFFFFFFFu, vs[0], i & 31);
             const int ahead = i + kStages;
@@ -158,7 +166,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
             const uint32_t at = count + i;
             const unsigned char* stage = ring + at % kStages * L::kStage;
             if (!dead && !mbar_wait_warp(bars + at % kStages, at / kStages & 1, a.status)) dead = true;
-            const int s0 = key0 + i * kFewKeys;              // first slot of the block
+            const int s0 = key0 + i * L::kKeys;              // first slot of the block
             // scores: rows x keys, key 4 (n >> 1) + 2 half + (n & 1) as column n of each half
             float s[2][4];
 #pragma unroll
@@ -286,17 +294,17 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
         float* part = a.parts + (long long)kv_slot(r, blockIdx.x) * kv_part_floats<kRows, D>();
         constexpr int kStride = kRows * D + 2 * kRows;
         const float* all = reinterpret_cast<const float*>(smem);
-        for (int at = threadIdx.x; at < kRows * D / 4; at += kFewThreads) {
+        for (int at = threadIdx.x; at < kRows * D / 4; at += L::kThreads) {
             const int row = at / (D / 4), d = at % (D / 4) * 4;
             if (row >= rows) break;
             float mm = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) mm = fmaxf(mm, all[w * kStride + kRows * D + row]);
+            for (int w = 0; w < L::kWarps; ++w) mm = fmaxf(mm, all[w * kStride + kRows * D + row]);
             const float base = mm == -INFINITY ? 0.f : mm;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             float ll = 0.f;
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) {
+            for (int w = 0; w < L::kWarps; ++w) {
                 const float f = ex2_approx(all[w * kStride + kRows * D + row] - base);
                 const float4 y = *reinterpret_cast<const float4*>(all + w * kStride + row * D + d);
                 ll += f * all[w * kStride + kRows * D + kRows + row];
@@ -314,8 +322,8 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 2 : 1) kv_attend_few_ke
         }
         if (cut) {
             if (threadIdx.x == 0) reinterpret_cast<int*>(part)[kRows * D + 2 * kRows] = any_nan;
-            if (kv_last_part<0, kFewThreads>(a.arrived + r.first, r.last - r.first + 1, word))
-                kv_join<kRows, D, T>(a, r, a.parts, 1, r.rt * kRows, rows, warp, kFewWarps);
+            if (kv_last_part<0, L::kThreads>(a.arrived + r.first, r.last - r.first + 1, word))
+                kv_join<kRows, D, T>(a, r, a.parts, 1, r.rt * kRows, rows, warp, L::kWarps);
         }
         proxy_fence();                                       // the ring is free again, for copies too
         __syncthreads();
