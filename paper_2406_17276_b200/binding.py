@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -43,23 +44,6 @@ class HostOut(C.Structure):
 class KVConfig(C.Structure):
     _fields_ = [(f, C.c_int32) for f in ("q_heads", "kv_heads", "head_dim", "page", "num_pages", "max_pages", "max_batch", "max_step",
                                          "layers", "dtype")]
-
-
-class KVCacheC(C.Structure):
-    _fields_ = [(f, C.c_void_p) for f in ("k", "v", "k_scale", "v_scale", "block_table")]
-
-
-class KVStepC(C.Structure):
-    _fields_ = [("B", C.c_int32), ("T", C.c_int32)] + [(f, C.c_void_p) for f in ("kv_len", "nodes", "base_pos", "position_ids", "mask")]
-
-
-class KVRows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
-
-
-class KVTurn(C.Structure):
-    _fields_ = [("cos_sin", C.c_void_p), ("positions", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
-                ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float)]
 
 
 _lib = None
@@ -350,10 +334,14 @@ def _index(device: torch.device) -> int:
     return device.index if device.type == "cuda" else -1
 
 
+# The structures of opt_tree_kv_* as bytes: packed faster than ctypes fills a Structure, and handed over by their address.
+_CACHE, _STEP, _ROWS, _TURN = (struct.Struct(f).pack for f in ("@5P", "@2i5P", "@P3q", "@P3iPPf"))
+
+
 def _addr(t, name: str, dtype, shape, index: int):
-    """Address of a contiguous tensor of this type, shape and device; None for None."""
+    """Address of a contiguous tensor of this type, shape and device; 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
         return t.data_ptr()
     raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on device {index} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -363,16 +351,15 @@ class KVCache:
     """Cache tensors (torch owns the memory): k, v [layers][num_pages][kv_heads][page][head_dim] float8_e4m3fn, k_scale, v_scale
     [layers][num_pages][kv_heads] float32, block_table [B][max_pages] int32 (see opt_tree_kv_cache).  One object serves any number of calls."""
 
-    __slots__ = ("k", "v", "k_scale", "v_scale", "block_table", "shape", "table_shape", "index", "c", "c_addr")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "block_table", "shape", "table_shape", "index", "c")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor):
         shape, table, index = k.shape, block_table.shape, k.get_device()
         if len(shape) != 5 or len(table) != 2:
             raise ValueError("k: [layers][num_pages][kv_heads][page][head_dim], block_table: [B][max_pages]")
         scales = shape[:3]
-        self.c = KVCacheC(_addr(k, "k", _F8, shape, index), _addr(v, "v", _F8, shape, index), _addr(k_scale, "k_scale", _F32, scales, index),
-                          _addr(v_scale, "v_scale", _F32, scales, index), _addr(block_table, "block_table", _I32, table, index))
-        self.c_addr = C.addressof(self.c)
+        self.c = _CACHE(_addr(k, "k", _F8, shape, index), _addr(v, "v", _F8, shape, index), _addr(k_scale, "k_scale", _F32, scales, index),
+                        _addr(v_scale, "v_scale", _F32, scales, index), _addr(block_table, "block_table", _I32, table, index))
         self.k, self.v, self.k_scale, self.v_scale, self.block_table = k, v, k_scale, v_scale, block_table
         self.shape, self.table_shape, self.index = shape, table, index
 
@@ -386,14 +373,15 @@ class KVStep:
                  position_ids: torch.Tensor | None = None, mask: torch.Tensor | None = None):
         self.kv_len, self.nodes, self.base_pos, self.position_ids, self.mask = kv_len, nodes, base_pos, position_ids, mask
 
-    def c_struct(self, B: int, T: int, device: torch.device) -> KVStepC:
-        return self._struct(B, T, _index(device))
+    def c_struct(self, B: int, T: int, device: torch.device) -> bytes:
+        return self._pack(B, T, _index(device))
 
-    def _struct(self, B: int, T: int, index: int) -> KVStepC:
-        one = (B,)
-        return KVStepC(B, T, _addr(self.kv_len, "kv_len", _I32, one, index), _addr(self.nodes, "nodes", _I32, one, index),
-                       _addr(self.base_pos, "base_pos", _I32, one, index), _addr(self.position_ids, "position_ids", _I32, (B, T - 1), index),
-                       _addr(self.mask, "mask", _I64, (B, T - 1, (T + 62) // 64), index) if T > 1 else None)
+    def _pack(self, B: int, T: int, index: int) -> bytes:
+        one, nodes, base, pos, mask = (B,), self.nodes, self.base_pos, self.position_ids, self.mask
+        return _STEP(B, T, _addr(self.kv_len, "kv_len", _I32, one, index), 0 if nodes is None else _addr(nodes, "nodes", _I32, one, index),
+                     0 if base is None else _addr(base, "base_pos", _I32, one, index),
+                     0 if pos is None else _addr(pos, "position_ids", _I32, (B, T - 1), index),
+                     0 if mask is None or T == 1 else _addr(mask, "mask", _I64, (B, T - 1, (T + 62) // 64), index))
 
 
 class TreeKV:
@@ -440,17 +428,16 @@ class TreeKV:
         ks, vs = (torch.ones((L, N, H), dtype=_F32, device=self.device) for _ in range(2))
         return KVCache(k, v, ks, vs, block_table)
 
-    def _rows(self, t: torch.Tensor, name: str, B: int, T: int, heads: int) -> KVRows:
+    def _rows(self, t: torch.Tensor, name: str, shape) -> bytes:
         st = t.stride()
-        if t.dtype is self.dtype and t.shape == (B, T, heads, self._D) and t.get_device() == self._at and st[3] == 1:
-            return KVRows(t.data_ptr(), st[0], st[1], st[2])
-        raise ValueError(f"{name}: {self.dtype} [{B}][{T}][{heads}][{self._D}] with contiguous rows on {self.device} is needed, "
-                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.dtype is self.dtype and t.shape == shape and t.get_device() == self._at and st[3] == 1:
+            return _ROWS(t.data_ptr(), st[0], st[1], st[2])
+        raise ValueError(f"{name}: {self.dtype} {tuple(shape)} with contiguous rows on {self.device} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
-    def _cache(self, cache: KVCache, B: int) -> int:
+    def _cache(self, cache: KVCache, B: int) -> bytes:
         table = cache.table_shape
         if cache.shape == self._cache_shape and cache.index == self._at and table[1] == self._max_pages and table[0] >= B:
-            return cache.c_addr
+            return cache.c
         raise ValueError(f"cache: pages {self._cache_shape} and a block table [{B}][{self._max_pages}] on {self.device} are needed, "
                          f"not {tuple(cache.shape)} and {tuple(table)} on {cache.k.device}")
 
@@ -470,34 +457,32 @@ class TreeKV:
                interleaved: bool = False, q_out: torch.Tensor | None = None) -> torch.Tensor | None:
         """opt_tree_kv_append: norm and rotation of q and k, k and v into the cache; returns the rotated queries (q_out; None if q is None)."""
         B, T = k.shape[:2]
-        at, rows, heads = self._at, self._rows, self._kv_heads
+        at, rows, D, each = self._at, self._rows, self._D, (B, T, self._kv_heads, self._D)
         qr = qo = None
         if q is not None:
+            shape = (B, T, self._q_heads, D)
             if q_out is None:
-                q_out = torch.empty((B, T, self._q_heads, self._D), dtype=self.dtype, device=self.device)
-            qr, qo = C.byref(rows(q, "q", B, T, self._q_heads)), C.byref(rows(q_out, "q_out", B, T, self._q_heads))
-        turn = KVTurn(None, 0, 0, bool(interleaved), None, None, eps)
-        if q_norm is not None:
-            turn.q_norm = _addr(q_norm, "q_norm", self.dtype, (self._D,), at)
-        if k_norm is not None:
-            turn.k_norm = _addr(k_norm, "k_norm", self.dtype, (self._D,), at)
+                q_out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            qr, qo = rows(q, "q", shape), rows(q_out, "q_out", shape)
+        angles, positions, rot = 0, 0, 0
         if cos_sin is not None:
-            turn.positions, turn.rot_dim = shape = cos_sin.shape
-            turn.cos_sin = _addr(cos_sin, "cos_sin", _F32, shape, at)
-        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, C.byref(rows(k, "k", B, T, heads)), C.byref(rows(v, "v", B, T, heads)), qo,
-                   C.byref(step._struct(B, T, at)), C.byref(turn))
+            positions, rot = cos_sin.shape
+            angles = _addr(cos_sin, "cos_sin", _F32, (positions, rot), at)
+        turn = _TURN(angles, positions, rot, 1 if interleaved else 0, 0 if q_norm is None else _addr(q_norm, "q_norm", self.dtype, (D,), at),
+                     0 if k_norm is None else _addr(k_norm, "k_norm", self.dtype, (D,), at), eps)
+        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, rows(k, "k", each), rows(v, "v", each), qo, step._pack(B, T, at), turn)
         return q_out
 
     def attend(self, cache: KVCache, layer: int, q: torch.Tensor, step: KVStep, scale: float | None = None, out: torch.Tensor | None = None,
                lse: torch.Tensor | None = None) -> torch.Tensor:
         """opt_tree_kv_attend: attention of the step's tokens over the cache; scale defaults to head_dim ** -0.5."""
         B, T = q.shape[:2]
-        heads = self._q_heads
+        heads, at = self._q_heads, self._at
+        shape = (B, T, heads, self._D)
         if out is None:
-            out = torch.empty((B, T, heads, self._D), dtype=self.dtype, device=self.device)
-        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, C.byref(self._rows(q, "q", B, T, heads)), C.byref(step._struct(B, T, self._at)),
-                   self._scale if scale is None else scale, C.byref(self._rows(out, "out", B, T, heads)),
-                   _addr(lse, "lse", _F32, (B, T, heads), self._at))
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, self._rows(q, "q", shape), step._pack(B, T, at), self._scale if scale is None else scale,
+                   self._rows(out, "out", shape), None if lse is None else _addr(lse, "lse", _F32, (B, T, heads), at))
         return out
 
     def compact(self, cache: KVCache, kv_len: torch.Tensor, kv_gather: torch.Tensor, kv_keep: torch.Tensor,

@@ -2,6 +2,7 @@
 graphs, on several streams, and over caches and batches of every size."""
 import ctypes as C
 import math
+import struct
 
 import numpy as np
 import pytest
@@ -239,7 +240,6 @@ def test_calls_too_large_to_count_are_refused():
     L, kv = binding.lib(), C.c_void_p()
     assert L.opt_tree_kv_create(C.byref(kv), C.byref(cfg)) == binding.OK
     some = torch.zeros(64, device="cuda").data_ptr()
-    cache, rows = binding.KVCacheC(some, some, some, some, some), binding.KVRows(some, 0, 0, 0)
-    step = binding.KVStepC(4096, 1, some, None, None, None, None)
-    assert L.opt_tree_kv_attend(kv, C.byref(cache), 0, C.byref(rows), C.byref(step), 1.0, C.byref(rows), None, None) == binding.ERR_UNSUPPORTED
+    cache, rows, step = struct.pack("@5P", *[some] * 5), struct.pack("@P3q", some, 0, 0, 0), struct.pack("@2i5P", 4096, 1, some, 0, 0, 0, 0)
+    assert L.opt_tree_kv_attend(kv, cache, 0, rows, step, 1.0, rows, None, None) == binding.ERR_UNSUPPORTED
     assert L.opt_tree_kv_launch_count(kv) == 0 and L.opt_tree_kv_destroy(kv) == binding.OK
