@@ -327,8 +327,14 @@ int opt_tree_kv_append(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t 
                        void *stream);
 
 /* out_i = sum_j softmax_j(scale * q_i . k_j) v_j over the slots that token i of the step sees, whose keys and values are in layer `layer`
- * of the cache (the step's own included: append first).
- *   q, out     rows of q_heads (q as opt_tree_kv_append wrote it); scale > 0, usually head_dim^-0.5
+ * of the cache (the step's own included: append first).  Products are taken in half precision, in which e4m3 codes are exact, and summed in
+ * single precision, as are softmax sums; probabilities are rounded to half precision (2^-11 of each at most).  Pages are brought to a
+ * common scale for that: values keep all their bits where their page's scale is at least 2^-15 of the largest among the slots that are read
+ * together, and 2^-25 of that largest below.  Rows that see a NaN are NaN (in the elements of a value that is NaN), others are not.
+ * Work is divided by what there is to read, whatever the lengths; results do not depend on how calls before or beside it went, but their
+ * last bits may depend on the other sequences of the batch, which decide where a sequence is cut.
+ * B * kv_heads * (row tiles of T) * (key tiles of max_pages * page) may not pass 2^30 (OPT_TREE_ERR_UNSUPPORTED).
+ *   q, out     rows of q_heads (q as opt_tree_kv_append wrote it); 0 < scale <= 1e38, usually head_dim^-0.5
  *   lse        (dev) [B][T][q_heads] float or NULL: log of the sum of exp(scale * q_i . k_j) */
 int opt_tree_kv_attend(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t layer, const opt_tree_kv_rows *q, const opt_tree_kv_step *step,
                        float scale, const opt_tree_kv_rows *out, float *lse, void *stream);

@@ -236,8 +236,10 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t four, uint32_t& seen) {
 // lines (row after row, each store of a warp touched 32 lines, and writing a tile's part took as long as four key tiles).
 template <int kRows, int D> __host__ __device__ constexpr int kv_part_floats() { return kRows * D + 2 * kRows + 4; }
 
-// A row's outputs at elements [d, d + N) of query row `row` of the run (row tile included).
-template <int D, int N, class T>
+template <int D, class T>
+__device__ __noinline__ void kv_mark_nan_call(const KvAttend& a, const KvRun& r, int row, int d, int n) { kv_mark_nan<D, T>(a, r, row, d, n); }
+// A row's outputs at elements [d, d + N) of query row `row` of the run (row tile included).  kCalls: the kernel may call functions.
+template <int D, int N, class T, bool kCalls = true>
 __device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int row, int d, const float (&x)[N], bool nan) {
     const int token = (int)a.by_group.div((unsigned)row), hq = r.h * a.group + row - token * a.group;
     uint16_t* to = const_cast<uint16_t*>(a.out.data) + r.b * a.out.batch + token * a.out.token + hq * a.out.head + d;
@@ -257,7 +259,10 @@ __device__ __forceinline__ void kv_store(const KvAttend& a, const KvRun& r, int 
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) *reinterpret_cast<uint32_t*>(to + 2 * i) = w[i];
     }
-    if (nan) kv_mark_nan<D, T>(a, r, row, d, N);
+    if (nan) {
+        if (kCalls) kv_mark_nan_call<D, T>(a, r, row, d, N);
+        else kv_mark_nan<D, T>(a, r, row, d, N);
+    }
 }
 __device__ __forceinline__ void kv_store_lse(const KvAttend& a, const KvRun& r, int row, float m, float l) {
     if (!a.lse) return;

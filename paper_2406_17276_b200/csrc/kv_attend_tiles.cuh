@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                         for (int i = 0; i < 8; ++i)
                             *reinterpret_cast<float4*>(part + ((c * 8 + i) * kTileRows + in_tile) * 4) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
                     } else {
-                        kv_store<D, 32, T>(a, r, row, c * 32, x, nan);
+                        kv_store<D, 32, T, false>(a, r, row, c * 32, x, nan);
                     }
                 }
                 if (mine && cut) { part[kTileRows * D + in_tile] = m; part[kTileRows * D + kTileRows + in_tile] = l; }

@@ -64,18 +64,26 @@ template <> __device__ __forceinline__ uint32_t from_float2<__half>(float lo, fl
     const __half2 r = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-// Eight consecutive elements; `wide`: the address is on a 16-byte boundary.
+// Eight consecutive elements; `wide`: the address is on a 16-byte boundary.  (The other way is a loop: it stands in many places, and code
+// that hardly ever runs should not fill the instruction cache.)
 __device__ __forceinline__ uint4 load8(const uint16_t* p, bool wide) {
-    if (wide) return *reinterpret_cast<const uint4*>(p);
     uint4 r;
-    r.x = p[0] | (uint32_t)p[1] << 16; r.y = p[2] | (uint32_t)p[3] << 16;
-    r.z = p[4] | (uint32_t)p[5] << 16; r.w = p[6] | (uint32_t)p[7] << 16;
+    if (wide) return *reinterpret_cast<const uint4*>(p);
+    r = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        r.x = __funnelshift_r(r.x, r.y, 16); r.y = __funnelshift_r(r.y, r.z, 16); r.z = __funnelshift_r(r.z, r.w, 16);
+        r.w = r.w >> 16 | (uint32_t)p[i] << 16;
+    }
     return r;
 }
 __device__ __forceinline__ void store8(uint16_t* p, uint4 v, bool wide) {
     if (wide) { *reinterpret_cast<uint4*>(p) = v; return; }
-    p[0] = (uint16_t)v.x; p[1] = (uint16_t)(v.x >> 16); p[2] = (uint16_t)v.y; p[3] = (uint16_t)(v.y >> 16);
-    p[4] = (uint16_t)v.z; p[5] = (uint16_t)(v.z >> 16); p[6] = (uint16_t)v.w; p[7] = (uint16_t)(v.w >> 16);
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        p[i] = (uint16_t)v.x;
+        v.x = __funnelshift_r(v.x, v.y, 16); v.y = __funnelshift_r(v.y, v.z, 16); v.z = __funnelshift_r(v.z, v.w, 16); v.w >>= 16;
+    }
 }
 template <class T> __device__ __forceinline__ void unpack8(uint4 v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
