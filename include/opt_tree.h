@@ -319,9 +319,10 @@ int opt_tree_kv_destroy(opt_tree_kv *kv);
  *   q, q_out   rows of q_heads, or both NULL; q_out may be q itself.  k, v: rows of kv_heads
  * Per page and head the scale becomes s = max(s_old, 2^max(-64, ceil(log2(a / 448)))) with a the largest magnitude of the step's entries
  * in it and s_old the page's scale if it holds older slots (below kv_len), else 0; older entries are brought to s (exactly, but
- * for those that become subnormal) and the new ones are e4m3(x / s), rounded to nearest even from single precision.  Infinite
- * inputs saturate and NaN stays NaN; neither sets the scale.  The page's rows behind the step's last are left as they were.
- * Norm and rotation are computed in single precision and q_out is rounded once; the scale is that of exact arithmetic. */
+ * for those that become subnormal) and the new ones are e4m3(x / s), rounded to nearest even.  Infinite inputs saturate and NaN stays
+ * NaN; neither sets the scale.  The page's rows behind the step's last are left as they were.
+ * Norm and rotation are computed in single precision and q_out is rounded once; where a scale or a code could come out otherwise than from the
+ * exact value, that value is taken again in double precision. */
 int opt_tree_kv_append(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t layer, const opt_tree_kv_rows *q, const opt_tree_kv_rows *k,
                        const opt_tree_kv_rows *v, const opt_tree_kv_rows *q_out, const opt_tree_kv_step *step, const opt_tree_kv_turn *turn,
                        void *stream);

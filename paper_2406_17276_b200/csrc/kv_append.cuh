@@ -7,7 +7,12 @@
 // The operator moves bytes: 2 read per element of q, k and v, 2 written per element of q, 1 per element of k and v.  One pass
 // needs the largest value of a whole page and head before anything can be written, so one CTA takes a page of one head and one
 // side (keys or values), keeps what it has read in registers, and writes after one reduction: no atomics, nothing is read twice.
-// Queries have no such tie and are spread over further CTAs of the same launch.
+// Queries have no such tie and are spread over further CTAs of the same launch, a warp for up to 16 heads (of 128 elements) of one token, so that
+// positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 114 us, for 4 x 4096 tokens of 32 / 8 heads of
+// 128, normed and rotated; 54 us would be the bytes at 6.5 TB/s).  What bounds it now: a CTA's life is a chain of loads (lengths, rows and
+// table, angles, scale) around little work, and the arithmetic of norm, rotation and conversion takes 60 % of the issue slots.  Queries
+// alone take 59 us (4.6 TB/s), pages alone 52 us.
+
 #pragma once
 
 #include "kv_common.cuh"
@@ -146,7 +151,7 @@ __device__ __forceinline__ void turn_exact(const KvAppend& a, const uint16_t* we
         for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        const double r = 1.0 / sqrt(sum / D + (double)a.eps);
+        const double r = rsqrt(sum * (1.0 / D) + (double)a.eps);
         unpack8<T>(load8(weights + sub * 8, a.wide_w), in);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = x[i] * r * in[i];
@@ -218,6 +223,12 @@ __device__ __forceinline__ float finite_abs(float x) {      // infinities satura
 __device__ __forceinline__ double finite_abs(double x) {
     const double m = fabs(x);
     return m <= 3.402823466e38 ? m : 0.0;
+}
+
+// A double as the float that rounds to the same code: cut off, with the last bit set if anything was.
+__device__ __forceinline__ float round_to_odd(double x) {
+    const float f = __double2float_rz(x);
+    return (double)f == x ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 
 // kPasses: row groups per warp that cover a page.
@@ -320,13 +331,47 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
         uint4* rows = reinterpret_cast<uint4*>(codes);
         for (int c = threadIdx.x; c < (lo - start) * (D / 16); c += kThreadsN) rows[c] = recode16(rows[c], ratio);
     }
+    // Single precision is off by less than 1.2e-6 of a pair's larger element (norm's sum and factor, folded weights, rotation; 4e-7 without
+    // a norm).  Rows with a value that near the middle between two codes are taken again in double precision below, so that what is
+    // stored is the rounding of the exact value.
+    const float tol = (a.k_norm ? 1.2e-6f : 4e-7f) * inv;
+    unsigned again = 0;                                                      // passes of this warp
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
-        if (r < n) {
+        if (turns && (i * kWarpsN + warp) * kRows < n) {                     // the same for the whole warp
+            float own = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) own = fmaxf(own, fabsf(x[i][c]));
+            own = tol * fmaxf(own, __shfl_sync(0xFFFFFFFFu, own, (lane & ~(kLanes - 1)) + partner));
+            float low[8];                                                    // rounding is monotone: codes of both ends tell
+#pragma unroll
+            for (int c = 0; c < 8; ++c) { low[c] = fmaf(x[i][c], inv, -own); x[i][c] = fmaf(x[i][c], inv, own); }
+            const uint2 under = make_uint2(to_e4m3x4(low[0], low[1], low[2], low[3]), to_e4m3x4(low[4], low[5], low[6], low[7]));
+            const uint2 over = make_uint2(to_e4m3x4(x[i][0], x[i][1], x[i][2], x[i][3]), to_e4m3x4(x[i][4], x[i][5], x[i][6], x[i][7]));
+            const bool near = ((under.x ^ over.x) | (under.y ^ over.y)) != 0;
+            again |= (__any_sync(0xFFFFFFFFu, near && r < n) ? 1u : 0u) << i;
+            if (r < n) *reinterpret_cast<uint2*>(codes + (long long)(lo - start + r) * D + sub * 8) = over;
+        } else if (r < n) {
             uint2 o;
             o.x = to_e4m3x4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
             o.y = to_e4m3x4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
+            *reinterpret_cast<uint2*>(codes + (long long)(lo - start + r) * D + sub * 8) = o;
+        }
+    }
+    while (again) {
+        const int i = __ffs(again) - 1, r = (i * kWarpsN + warp) * kRows + lane / kLanes;
+        again &= again - 1;
+        uint4 raw2 = make_uint4(0, 0, 0, 0);
+        if (r < n) raw2 = load8(from + (long long)(lo - len + r) * src.token, wide);
+        double y[8];
+        KvAngles g;
+        if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len, base), g);
+        turn_exact<D, T>(a, a.k_norm, g, sub, partner, raw2, y);
+        if (r < n) {
+            uint2 o;
+            o.x = to_e4m3x4(round_to_odd(y[0]) * inv, round_to_odd(y[1]) * inv, round_to_odd(y[2]) * inv, round_to_odd(y[3]) * inv);
+            o.y = to_e4m3x4(round_to_odd(y[4]) * inv, round_to_odd(y[5]) * inv, round_to_odd(y[6]) * inv, round_to_odd(y[7]) * inv);
             *reinterpret_cast<uint2*>(codes + (long long)(lo - start + r) * D + sub * 8) = o;
         }
     }

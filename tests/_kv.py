@@ -74,9 +74,7 @@ def sees(step, b, tokens):
 
 
 def append(codes, scale, table, step, x, page):
-    """One side of an append into values codes [pages][heads][page][D] and scale [pages][heads], in place.  x: [B][T][heads][D], turned.
-    Returns, for every new entry, x / s beside the value that was stored."""
-    pairs = []
+    """One side of an append into values codes [pages][heads][page][D] and scale [pages][heads], in place.  x: [B][T][heads][D], turned."""
     for b in range(len(step["len"])):
         n0, m = int(step["len"][b]), int(step["nodes"][b]) + 1
         for p in range(n0 // page, (n0 + m - 1) // page + 1) if m > 0 else []:
@@ -91,8 +89,6 @@ def append(codes, scale, table, step, x, page):
                     codes[i, h, :lo - p * page] = nearest(codes[i, h, :lo - p * page] * (scale[i, h] / s))
                 scale[i, h] = s
                 codes[i, h, lo - p * page:hi - p * page] = nearest(v / s)
-                pairs.append(((i, h, lo - p * page, hi - p * page), v / s))
-    return pairs
 
 
 def attend(k, v, ks, vs, table, step, q, scale, page):
