@@ -290,10 +290,10 @@ __device__ __forceinline__ bool kv_last_part(int* arrived, int pieces, int* word
     return *word != 0;
 }
 // Joins a cut row tile's parts in the order of the keys: a lane a row, a chunk of four elements at a time.  kStep: parts from one slot to
-// the next.  row0: the tile's first row.  Of the tile's groups of rows times chunks (kLanesOf lanes each) this warp does warp, warp + warps, ...
-template <int kRows, int D, class T>
-__device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
-    constexpr int kFloats = kv_part_floats<kRows, D>(), kChunks = D / 4, kAtOnce = kRows < 32 ? 16 : 8;      // parts in flight
+// the next.  row0: the tile's first row.  Of the tile's groups of rows times chunks this warp does warp, warp + warps, ...  kAtOnce: parts in flight.
+template <int kRows, int D, class T, int kAtOnce>
+__device__ __forceinline__ void kv_join_by(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
+    constexpr int kFloats = kv_part_floats<kRows, D>(), kChunks = D / 4;
     constexpr int kLaneRows = kRows < 32 ? kRows : 32, kLaneChunks = 32 / kLaneRows;
     const int lane = threadIdx.x & 31, pieces = r.last - r.first + 1;
     const long long step = (long long)kStep * kFloats;
@@ -342,6 +342,13 @@ __device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const
             if (chunk == 0) kv_store_lse(a, r, row0 + row, top, l);
         }
     }
+}
+
+// (Two parts are the rule where there is much to do, many where there is little.)
+template <int kRows, int D, class T>
+__device__ __forceinline__ void kv_join(const KvAttend& a, const KvRun& r, const float* parts, int kStep, int row0, int rows, int warp, int warps) {
+    if (r.last - r.first < 2) kv_join_by<kRows, D, T, 2>(a, r, parts, kStep, row0, rows, warp, warps);
+    else kv_join_by<kRows, D, T, kRows < 32 ? 16 : 8>(a, r, parts, kStep, row0, rows, warp, warps);
 }
 
 }  // namespace ot
