@@ -2,21 +2,25 @@
 //
 // Per tile of 128 keys: S = Q K^T (tcgen05, both operands from shared memory, fp32 in TMEM), softmax by the threads that own the rows, P in
 // half precision back to TMEM over S, O += P V with P from TMEM.  Two row tiles of 128 alternate, so that the tensor cores
-// work on one while the other's exponentials are taken.  Keys and values become half precision on their way into shared memory, where
-// e4m3 codes are exact: four warps load codes, convert, bring them to the largest page scale of the run (a power of two: exact
-// to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once per 256 rows.  (Eight-bit operands would need
-// queries and probabilities in two parts each: the same tensor time as half precision, and twice the conversions per row.)
-// One exponent per score: 16 a clock and SM, as long as both products of a tile take (2 * 128 * 128 * D at 4096 a clock for D =
-// 128); so neither side can be hidden behind the other much further.
+// work on one while the other's exponentials are taken; a row tile that is alone is shared by both softmax groups, which take its key tiles in turn.
+// Keys and values become half precision on their way into shared memory, where e4m3 codes are exact: four warps a side load codes, convert,
+// bring them to a common page scale (a power of two: exact to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once
+// per 256 rows.  (Eight-bit operands would need queries and probabilities in two parts each: the same tensor time as half precision, and
+// twice the conversions per row.)
+// What bounds it: the chain of a key tile (codes, conversion, scores, exponentials, values), no unit by itself.  32 trees of 65 tokens over 4096
+// slots, 32 / 8 heads of 128: 198 us, 470 TFLOP/s; the exponentials alone would take 40 us, the products 56.
 //
-// Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 conversion; warp 12 issues the products; warp 13 looks pages up and
-// copies their codes into shared memory a key tile ahead.  Barriers (all waits bounded):
+// Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 convert keys, 12-15 values; warp 16 issues the products; warp 17 divides the
+// work, looks pages up and copies their codes into shared memory a key tile ahead; two warps fill the last warpgroup.  Barriers (all waits bounded;
+// a role whose wait ran out waits for nothing more and leaves, and the others' waits run out after it):
+//   run[8]     copies -> all            what to do next
 //   q          softmax -> products      queries of a run are in shared memory
 //   rk, rv     copies <-> conversion    codes of a key tile
 //   k, v       conversion <-> products  operands, two stages each
 //   s[X][2]    products -> softmax X    scores of half a key tile: one half's are ready while the other's exponentials are taken
 //   p[X][2]    softmax X -> products
 //   o[X][2]    products -> softmax X    O holds the values of half a key tile (waited for before O is rescaled, and at the end)
+// and named barrier 1 between the softmax groups: sums of a shared row tile handed over, and its outputs read.
 #pragma once
 
 #include <type_traits>
@@ -112,9 +116,11 @@ struct TileInfo {
     float kmax, ref;                     // largest scale of the keys, reference of the values
     float pad[2];
 };
-// Slots of TileInfo, by tile, and of the runs and their NaN words, by run.  The copying warp writes those of tile t (of run r) once the codes of tile t - 2 at
-// least have been taken; then values of t - 3 have been written, so the products of t - 5 are complete, so both softmax groups are done with
-// tile t - 5, and done with the run before that tile's.
+// Slots of TileInfo, by tile, and of the runs and their NaN words, by run.  The copying warp writes those of tile t (of run r) once the codes
+// of keys of tile t - 2 at least have been taken.  Then keys of t - 3 have been written, so the scores of t - 5 are complete; those were
+// issued after the values of tile t - 7 (t - 6 with two row tiles) had been added up.  So both softmax groups, and the conversion of values, are done with tile
+// t - 7, and the groups with the run before that tile's.  (A run is published a tile earlier than that: its slot was taken at the start of the run that
+// used it, which has to be over by t - 8.)
 constexpr int kTileSlots = 8;
 
 template <int D> struct TileLayout {
@@ -124,8 +130,7 @@ template <int D> struct TileLayout {
     static constexpr int kBars = kRawV + kRaw * kCodes;
     enum { kBarQ, kBarKFull, kBarKFree = kBarKFull + 2, kBarVFull = kBarKFree + 2, kBarVFree = kBarVFull + 2, kBarS = kBarVFree + 2, kBarP = kBarS + 4,
            kBarO = kBarP + 4, kBarRKFull = kBarO + 4, kBarRKFree = kBarRKFull + kRaw, kBarRVFull = kBarRKFree + kRaw, kBarRVFree = kBarRVFull + kRaw,
-           kBarRun = kBarRVFree + kRaw,
-           kBarEnd = kBarRun + kTileSlots, kBarCount };
+           kBarRun = kBarRVFree + kRaw, kBarEnd = kBarRun + kTileSlots, kBarCount };
     static constexpr int kInfo = (kBars + kBarCount * 8 + 15) & ~15, kNan = kInfo + kTileSlots * (int)sizeof(TileInfo), kWord = kNan + kTileSlots * 4, kMerge = kWord + 16,
                          kRuns = kMerge + 1024 + 16;
     static constexpr int kBytes = kRuns + kTileSlots * (int)sizeof(KvRun);
@@ -209,8 +214,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_wait();
-    // A wait that runs out is recorded; from then on this warp waits for nothing more but goes through its work, so that barriers and
-    // counters stay in step and the kernel ends.
+    // A wait that runs out is recorded; this warp waits for nothing more then and leaves at the end of its run (softmax: of all runs).
     bool dead = false;
     auto wait = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_warp(bars + bar, parity, a.status); };
     KvRun r;
@@ -231,7 +235,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         const uint32_t ts = lanes + L::kColS + X * 128, to = lanes + L::kColO + X * D;
         uint32_t tiles = 0, at = 0;                          // key tiles of this group, and of the runs before
         int run = 0;
-        while (next_run(wait)) {
+        // Both groups go through all runs, also when a wait has run out (it is the last one then), so that neither misses the other at the
+        // named barrier; the copying warp gives the last run out in any case, later by a wait of its own at most.
+        auto next = [&] {
+            const int slot = runs_taken & (kTileSlots - 1);
+            const bool there = mbar_wait_warp(bars + L::kBarRun + slot, runs_taken / kTileSlots & 1, a.status, 8 * kWaitCycles);
+            ++runs_taken;
+            r = runs[slot];
+            return there && r.b >= 0;
+        };
+        while (next()) {
             const bool single = r.tokens * a.group - r.rt * 2 * kTileRows <= kTileRows;
             const int row0 = r.rt * 2 * kTileRows + (single ? 0 : X * kTileRows), rows = min(kTileRows, r.tokens * a.group - row0);
             const int row = row0 + in_tile;
@@ -466,7 +479,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             for (int kt = r.k0; kt < r.k1; ++kt, ++done) {
                 const uint32_t stage = done & 1, phase = done >> 1 & 1, st = done % L::kRaw, raw_phase = done / L::kRaw & 1;
                 const TileInfo& info = infos[done & (kTileSlots - 1)];
-                {
+                {                                            // (the same code for both sides)
                     const int raw_full = side ? L::kBarRVFull : L::kBarRKFull, raw_free = side ? L::kBarRVFree : L::kBarRKFree;
                     const int full = side ? L::kBarVFull : L::kBarKFull, free_ = side ? L::kBarVFree : L::kBarKFree;
                     const unsigned char* from = smem + (side ? L::kRawV : L::kRawK) + st * L::kCodes + tid * 16;
