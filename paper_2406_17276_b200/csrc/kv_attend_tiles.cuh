@@ -7,8 +7,8 @@
 // bring them to a common page scale (a power of two: exact to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once
 // per 256 rows.  (Eight-bit operands would need queries and probabilities in two parts each: the same tensor time as half precision, and
 // twice the conversions per row.)
-// What bounds it: the chain of a key tile (codes, conversion, scores, exponentials, values), no unit by itself.  32 trees of 65 tokens over 4096
-// slots, 32 / 8 heads of 128: 198 us, 470 TFLOP/s; the exponentials alone would take 40 us, the products 56.
+// What bounds it: the chain of a key tile (codes, conversion, scores, exponentials, values), no unit by itself.  32 trees of 65 tokens over up to 4096
+// slots, 32 / 8 heads of 128: 197 us, 470 TFLOP/s; the exponentials alone would take 40 us, the products 56.
 //
 // Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 convert keys, 12-15 values; warp 16 issues the products; warp 17 divides the
 // work, looks pages up and copies their codes into shared memory a key tile ahead; two warps fill the last warpgroup.  Barriers (all waits bounded;

@@ -62,6 +62,11 @@ def test_trees(D, page, dtype, n):
     run(_kv.Case([0, 1, 127, 128, 200, 31], [n, n - 1, n // 2, n, 0, -1], n + 1, D=D, page=page, dtype=dtype, hq=8, hkv=2, seed=page + D + n))
 
 
+@pytest.mark.parametrize("n,D,page,dtype,hq,hkv", [(300, 128, 32, BF, 6, 2), (640, 64, 16, HF, 2, 2), (1024, 128, 128, HF, 2, 1), (1024, 64, 64, BF, 3, 3)])
+def test_trees_of_many_words(n, D, page, dtype, hq, hkv):
+    run(_kv.Case([5, 0, 260, 1000], [n, n // 2 + 1, 63, 64], n + 1, D=D, page=page, dtype=dtype, hq=hq, hkv=hkv, seed=n + D))
+
+
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (7, 1), (12, 4), (16, 1), (33, 1), (64, 2), (5, 5)])
 def test_heads(hq, hkv):
     run(_kv.Case([100, 9], [0, 0], 1, hq=hq, hkv=hkv, D=128, seed=hq))
