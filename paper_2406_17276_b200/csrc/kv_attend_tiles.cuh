@@ -408,8 +408,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             const bool cut = r.first != r.last;
             constexpr int kFloats = kv_part_floats<kTileRows, D>();
             float* part = a.parts + ((long long)kv_slot(r, blockIdx.x) * 2 + (single ? 0 : X)) * kFloats;
-            const bool nan = nans[run & (kTileSlots - 1)] != 0;
-            ++run;
             // a single row tile: the first group takes the second's sums, and reads its outputs from TMEM
             const bool both = single && r.k1 - r.k0 > 1;
             float mine_f = ref, other_f = 0.f;
@@ -431,6 +429,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     m = mm;
                 }
             }
+            // (behind the barrier: of a single row tile, the run's last values may be the second group's, which has waited for their products)
+            const bool nan = nans[run & (kTileSlots - 1)] != 0;
+            ++run;
             const float norm = cut ? 1.f : 1.f / l;
             mine_f *= norm; other_f *= norm;
             if (busy && (!single || X == 0)) {

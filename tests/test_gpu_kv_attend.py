@@ -194,3 +194,20 @@ def test_sizes_and_pages_out_of_range_are_recorded():
         kv.attend(binding.KVCache(*tensors), 0, q, step, None, out)
         assert kv.device_status() == binding.ERR_INTERNAL and kv.device_status() == 0
         assert torch.isfinite(out[1].float()).all() and not (out[1] == 77.0).any()          # the other sequence is served
+
+
+@pytest.mark.parametrize("tiles", [2, 3, 4, 5, 7])
+@pytest.mark.parametrize("B,hkv", [(1, 1), (60, 4)])
+def test_nan_values_in_every_key_tile_of_a_single_row_tile(tiles, B, hkv):
+    """70 rows per key head, a step that lies in the last two tiles of 128 keys: whichever of the two groups takes the NaN, and whether
+    the row tile is cut or not, the rows that see it are NaN and no others."""
+    T = 70
+    case = _kv.Case([128 * (tiles - 1) - 30 + b % 2 * 35 for b in range(B)], [T - 1] * B, T, hq=hkv, hkv=hkv, D=64, page=32, seed=tiles)
+    tensors = case.cache()
+    for j in (3, 68):                                          # the first one before the last tile, in every other sequence
+        for b in range(B):
+            s = int(case.step["len"][b]) + j
+            tensors[1].view(torch.uint8)[0, int(case.table[b, s // case.page]), :, s % case.page, 5 + j % 2] = 0x7F
+    q = case.rows(case.hq, 2.0)
+    for _ in range(5):
+        run(case, tensors=tensors, q=q, with_lse=False)
