@@ -4,7 +4,7 @@
 // half precision back to TMEM over S, O += P V with P from TMEM.  Two row tiles of 128 alternate, so that the tensor cores
 // work on one while the other's exponentials are taken; a row tile that is alone is shared by both softmax groups, which take its key tiles in turn.
 // Keys and values become half precision on their way into shared memory, where e4m3 codes are exact: four warps a side load codes, convert,
-// bring them to a common page scale (a power of two: exact to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once
+// bring them to a common page scale (by powers of two: exact to 2^-15 of it, rounded to 2^-25 of it below) and write the swizzled layout; once
 // per 256 rows.  (Eight-bit operands would need queries and probabilities in two parts each: the same tensor time as half precision, and
 // twice the conversions per row.)
 // What bounds it: the chain of a key tile (codes, conversion, scores, exponentials, values), no unit by itself.  32 trees of 65 tokens over up to 4096
@@ -96,6 +96,23 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16
                  ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]),
                    "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
 }
+// The same of 16 columns, and a store of eight.
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&x)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]),
+                   "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_wait16(float (&x)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]), "+f"(x[9]),
+                   "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&x)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+}
 // One lane of a converged warp, always the same one.  (Asked by elect.sync and not by the lane's number, the compiler knows that a single
 // thread is left, and hands the tensor instructions their operands without asking every lane for its own.)
 __device__ __forceinline__ bool elect_one() {
@@ -108,14 +125,23 @@ __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait:
 // fp32 accumulators, half-precision operands, M = 128; mn: the second operand is MN-major.
 __host__ __device__ constexpr uint32_t tc_idesc(int n, bool mn) { return 1u << 4 | (mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24; }
 
-// What the copying warp finds out about a key tile.  Keys of a tile are brought to the tile's largest scale, values to one reference that
-// outputs are kept in: the first tile's largest scale, or a later one's that is over 64 times the reference so far (64 * 448 is within
+// What the copying warp finds out about a key tile.  A scale is taken as a power of two, which the operands are brought to in half precision
+// without a rounding, times a fraction, which scores and probabilities are multiplied by in single precision (half precision's rounding of a scale
+// would shift all scores of a page alike).  Fractions other than 1 are dealt with apart, in loops that are not unrolled: that they may come at all
+// takes 3 % of a call without any (195 -> 201 us, 296 -> 304 us for the batches below); multiplied in where the scores are in registers, 8 to 18 %.  Keys of a tile are brought to the tile's largest power, values to one reference that
+// outputs are kept in: the first tile's largest power, or a later one's that is over 64 times the reference so far (64 * 448 is within
 // half precision).
-struct TileInfo {
-    uint32_t kratio[8], vratio[8];       // of each 16 keys, twice in half precision
-    float kmax, ref;                     // largest scale of the keys, reference of the values
-    float pad[2];
+struct alignas(16) TileHead {
+    float kmax, ref;                     // largest power of the keys, reference of the values
+    int odd, pad;                        // fractions other than 1: of keys (1), of values (2)
 };
+struct TileInfo {
+    uint32_t kratio[8], vratio[8];       // of each 16 keys: the power over the tile's, twice in half precision
+    float kfrac[8], vfrac[8];            // of each 16 keys: the fraction
+    TileHead head;
+};
+// The smallest power of two that is no smaller than a scale (2^127 above it, 2^-126 for subnormal scales; 0 for 0).
+__device__ __forceinline__ float scale_power(float s) { return __uint_as_float(min((__float_as_uint(s) + 0x7FFFFFu) & 0x7F800000u, 0x7F000000u)); }
 // Slots of TileInfo, by tile, and of the runs and their NaN words, by run.  The copying warp writes those of tile t (of run r) once the codes
 // of keys of tile t - 2 at least have been taken.  Then keys of t - 3 have been written, so the scores of t - 5 are complete; those were
 // issued after the values of tile t - 7 (t - 6 with two row tiles) had been added up.  So both softmax groups, and the conversion of values, are done with tile
@@ -137,6 +163,8 @@ template <int D> struct TileLayout {
     static constexpr uint32_t kColumns = 512, kColS = 0, kColO = 256;
 };
 static_assert(TileLayout<128>::kBytes <= 227 * 1024, "shared memory of a CTA");
+// 1 / p of a power of two of scale_power (2^-126 ... 2^127); something finite for 0.
+__device__ __forceinline__ float power_inverse(float p) { return __uint_as_float(max(0x7F000000u - __float_as_uint(p), 0x00400000u)); }
 
 // Bits of the slots that token i of a run's sequence sees among the step's tokens [j0, j0 + 64) (negative j: the prefix).
 __device__ __forceinline__ uint64_t kv_sees64(const KvStep& st, int b, int i, int tokens, int j0) {
@@ -327,14 +355,32 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     tc_fence_after();
                     if (busy) {
                         const uint32_t from = ts + half * 64;
-                        const float f = fmaxf(qf * info.kmax, 1.2e-38f);
-                        const float unit = ref == info.ref ? 1.f : ref / info.ref;
-                        ref = info.ref;
+                        const TileHead head = info.head;
+                        const float f = fmaxf(qf * head.kmax, 1.2e-38f);
+                        const float unit = ref == head.ref ? 1.f : ref / head.ref;
+                        ref = head.ref;
                         float x[2][32];
                         tmem_load(from, x[0]);
                         tmem_load(from + 32, x[1]);
                         tmem_wait(x[0]);
                         tmem_wait(x[1]);
+                        if (__builtin_expect(head.odd & 1, 0)) {               // fractions of key scales
+#pragma unroll 1
+                            for (int g = 0; g < 4; ++g) {
+                                float y[16];
+                                tmem_load16(from + g * 16, y);
+                                tmem_wait16(y);
+                                uint32_t z[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) z[i] = __float_as_uint(y[i] * info.kfrac[half * 4 + g]);
+                                tmem_store16(from + g * 16, z);
+                            }
+                            tmem_wait_stores();
+                            tmem_load(from, x[0]);
+                            tmem_load(from + 32, x[1]);
+                            tmem_wait(x[0]);
+                            tmem_wait(x[1]);
+                        }
                         if (edge) {
 #pragma unroll
                             for (int c = 0; c < 2; ++c)
@@ -375,18 +421,39 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                         const float base = !(top < INFINITY) ? __int_as_float(0x7FC00000) : (m == -INFINITY ? 0.f : m);
                         const unsigned long long f2 = pack2(f, f), base2 = pack2(-base, -base);
                         unsigned long long sum[2] = {0ull, 0ull};
+                        if (__builtin_expect(!(head.odd & 2), 1)) {
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t p[16];
+                            for (int c = 0; c < 2; ++c) {
+                                uint32_t p[16];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float e0, e1;
-                                unpack2(fma2(pack2(x[c][2 * i], x[c][2 * i + 1]), f2, base2), e0, e1);
-                                e0 = ex2_approx(e0); e1 = ex2_approx(e1);
-                                sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
-                                p[i] = from_float2<__half>(e0, e1);
+                                for (int i = 0; i < 16; ++i) {
+                                    float e0, e1;
+                                    unpack2(fma2(pack2(x[c][2 * i], x[c][2 * i + 1]), f2, base2), e0, e1);
+                                    e0 = ex2_approx(e0); e1 = ex2_approx(e1);
+                                    sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+                                    p[i] = from_float2<__half>(e0, e1);
+                                }
+                                tmem_store16(from + c * 16, p);
                             }
-                            tmem_store16(from + c * 16, p);
+                        } else {                             // fractions of value scales: 16 scores at a time, read again (P(g) only covers scores that have been)
+#pragma unroll 1
+                            for (int g = 0; g < 4; ++g) {
+                                const float vfrac = info.vfrac[half * 4 + g];
+                                float y[16];
+                                tmem_load16(from + g * 16, y);
+                                tmem_wait16(y);
+                                uint32_t p[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    float e0, e1;
+                                    unpack2(fma2(pack2(y[2 * i], y[2 * i + 1]), f2, base2), e0, e1);
+                                    e0 = ex2_approx(!edge || see >> (g * 16 + 2 * i) & 1 ? e0 : -INFINITY);
+                                    e1 = ex2_approx(!edge || see >> (g * 16 + 2 * i + 1) & 1 ? e1 : -INFINITY);
+                                    sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+                                    p[i] = from_float2<__half>(e0 * vfrac, e1 * vfrac);
+                                }
+                                tmem_store8(from + g * 8, p);
+                            }
                         }
                         float s0, s1;
                         unpack2(add2(sum[0], sum[1]), s0, s1);
@@ -570,7 +637,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 // lanes 0 to 7: this tile's groups of 16 keys
                 const int from = (n & 3) * 8 + (lane & 7);
                 const int mine = __shfl_sync(0xFFFFFFFFu, id[0], from);
-                const float k = __shfl_sync(0xFFFFFFFFu, ks[0], from), v = __shfl_sync(0xFFFFFFFFu, vs[0], from);
+                const float kscale = __shfl_sync(0xFFFFFFFFu, ks[0], from), vscale = __shfl_sync(0xFFFFFFFFu, vs[0], from);
+                const float k = scale_power(kscale), v = scale_power(vscale);
+                const float kfrac = kscale * power_inverse(k), vfrac = vscale * power_inverse(v);
+                const int odd = (__any_sync(0xFFFFFFFFu, kscale != k) ? 1 : 0) | (__any_sync(0xFFFFFFFFu, vscale != v) ? 2 : 0);
                 const float kmax = warp_max_f32(k), vmax = warp_max_f32(v);
                 if (n == 0 || vmax > 64.f * ref) ref = vmax;
                 const int s = kt * kTileKeys + lane * 16;
@@ -581,11 +651,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 wait(L::kBarRKFree + st, phase ^ 1);
                 if (lane < 8) {
                     TileInfo& info = infos[done & (kTileSlots - 1)];
-                    const __half2 kr = __float2half2_rn(kmax > 0.f ? k / kmax : 0.f), vr = __float2half2_rn(ref > 0.f ? v / ref : 0.f);
+                    const __half2 kr = __float2half2_rn(k * power_inverse(kmax)), vr = __float2half2_rn(v * power_inverse(ref));
                     info.kratio[lane] = *reinterpret_cast<const uint32_t*>(&kr);
                     info.vratio[lane] = *reinterpret_cast<const uint32_t*>(&vr);
+                    info.kfrac[lane] = kfrac; info.vfrac[lane] = vfrac;
                     if (lane == 0) {
-                        info.kmax = kmax; info.ref = ref;
+                        info.head = TileHead{kmax, ref, odd, 0};
                         if (n == 0) nans[run & (kTileSlots - 1)] = 0;
                     }
                 }

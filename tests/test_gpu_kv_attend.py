@@ -211,3 +211,16 @@ def test_nan_values_in_every_key_tile_of_a_single_row_tile(tiles, B, hkv):
     q = case.rows(case.hq, 2.0)
     for _ in range(5):
         run(case, tensors=tensors, q=q, with_lse=False)
+
+
+@pytest.mark.parametrize("T", [1, 7, 30, 80, 150])
+@pytest.mark.parametrize("side,spread", [("both", 2.0), ("keys", 4.0), ("values", 1.0)])
+def test_scales_with_a_fraction_of_their_own(T, side, spread):
+    """Every page and head has a scale of its own that is no power of two: both kernels, single and double row tiles."""
+    for D, hq, hkv in ((64, 8, 2), (128, 3, 3)):
+        case = _kv.Case([290, 60, 7], [T - 1, T // 2, T - 1], T, D=D, hq=hq, hkv=hkv, seed=20 + T)
+        tensors = case.cache()
+        for which, t in (("keys", tensors[2]), ("values", tensors[3])):
+            if side in ("both", which):
+                t.mul_(torch.from_numpy(case.rs.uniform(1.0, 2.0, tuple(t.shape))).float().cuda())
+        run(case, tensors=tensors, spread=spread)
