@@ -5,7 +5,7 @@
 // All query rows of a sequence that read one key head (tokens x query heads per key head, token-major) are taken together, so that
 // a page is read and converted once for them.  Work is cut by the clock and not by sequence: the tiles (sequence, key head, row
 // tile, tile of keys) are numbered in that order and every CTA takes an equal run of them, whatever the lengths; a row tile that is cut
-// leaves its parts (maximum, sum, unnormalised output) in the workspace, and the CTA that finishes last joins them in order, so
+// leaves its parts (maximum, sum, output) in the workspace, and the CTA that finishes last joins them in order, so
 // results do not depend on who that is.
 #pragma once
 
@@ -231,8 +231,8 @@ __device__ __forceinline__ uint32_t drop_nan(uint32_t four, uint32_t& seen) {
     return four & ~nan;
 }
 
-// A cut row tile's part: kRows x D unnormalised outputs (values' scales applied), then maxima, sums and a word that says whether
-// NaN values were met.  Outputs lie in chunks of four elements, [D / 4][kRows][4], so that threads with a row each write and read whole
+// A cut row tile's part: kRows x D outputs over the part's keys alone (divided by its sum, so that large values stay within single precision however
+// many keys there are), then maxima, sums and a word that says whether NaN values were met.  Outputs lie in chunks of four elements, [D / 4][kRows][4], so that threads with a row each write and read whole
 // lines (row after row, each store of a warp touched 32 lines, and writing a tile's part took as long as four key tiles).
 template <int kRows, int D> __host__ __device__ constexpr int kv_part_floats() { return kRows * D + 2 * kRows + 4; }
 
@@ -321,22 +321,24 @@ __device__ __forceinline__ void kv_join_by(const KvAttend& a, const KvRun& r, co
             const float was = top;
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
-            const float bottom = top == -INFINITY ? 0.f : top, fade = ex2_approx(was - bottom);
-            l *= fade;
+            const float bottom = top == -INFINITY ? 0.f : top, before = l * ex2_approx(was - bottom);
+            l = before;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] *= fade;
+            for (int k = 0; k < kAtOnce; ++k) {
+                s[k] = i + k < pieces ? s[k] * ex2_approx(m[k] - bottom) : 0.f;
+                l += s[k];
+            }
+            const float over = l == 0.f ? 0.f : 1.f / l, keep = before * over;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] *= keep;
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k)
                 if (i + k < pieces) {
-                    const float f = ex2_approx(m[k] - bottom);
-                    l += f * s[k];
+                    const float f = s[k] * over;
                     x[0] += f * y[k].x; x[1] += f * y[k].y; x[2] += f * y[k].z; x[3] += f * y[k].w;
                 }
         }
         if (top == -INFINITY) top = 0.f;
-        const float f = 1.f / l;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] *= f;
         if (row < rows) {
             kv_store<D, 4, T>(a, r, row0 + row, chunk * 4, x, nan);
             if (chunk == 0) kv_store_lse(a, r, row0 + row, top, l);

@@ -280,9 +280,10 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
             l[n] += __shfl_xor_sync(0xFFFFFFFFu, l[n], 1);
             l[n] += __shfl_xor_sync(0xFFFFFFFFu, l[n], 2);
             if (t == 0) { mo[kRows * D + n * 8 + g] = m[n]; mo[kRows * D + kRows + n * 8 + g] = l[n]; }
-            const float unit = ref * (1.f / kProbUnit);
+            const float over = l[n] > 0.f ? 1.f / l[n] : 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {                    // row 2t + e: this lane's D/8 consecutive elements
+                const float unit = ref * (1.f / kProbUnit) * __shfl_sync(0xFFFFFFFFu, over, 8 * t + 4 * e);
                 float* to = mo + (n * 8 + 2 * t + e) * D + g * (D / 8);
 #pragma unroll
                 for (int d = 0; d < kSteps; d += 2)
@@ -302,20 +303,24 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
             for (int w = 0; w < L::kWarps; ++w) mm = fmaxf(mm, all[w * kStride + kRows * D + row]);
             const float base = mm == -INFINITY ? 0.f : mm;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float ll = 0.f;
+            float ll = 0.f, share[L::kWarps];
 #pragma unroll
             for (int w = 0; w < L::kWarps; ++w) {
-                const float f = ex2_approx(all[w * kStride + kRows * D + row] - base);
+                share[w] = ex2_approx(all[w * kStride + kRows * D + row] - base) * all[w * kStride + kRows * D + kRows + row];
+                ll += share[w];
+            }
+            const float over = ll > 0.f ? 1.f / ll : 0.f;
+#pragma unroll
+            for (int w = 0; w < L::kWarps; ++w) {
+                const float f = share[w] * over;
                 const float4 y = *reinterpret_cast<const float4*>(all + w * kStride + row * D + d);
-                ll += f * all[w * kStride + kRows * D + kRows + row];
                 sum.x += f * y.x; sum.y += f * y.y; sum.z += f * y.z; sum.w += f * y.w;
             }
             if (cut) {
                 *reinterpret_cast<float4*>(part + (d / 4 * kRows + row) * 4) = sum;
                 if (d == 0) { part[kRows * D + row] = mm; part[kRows * D + kRows + row] = ll; }
             } else {
-                const float f = 1.f / ll;
-                float x[4] = {sum.x * f, sum.y * f, sum.z * f, sum.w * f};
+                const float x[4] = {sum.x, sum.y, sum.z, sum.w};
                 kv_store<D, 4, T>(a, r, r.rt * kRows + row, d, x, any_nan);
                 if (d == 0) kv_store_lse(a, r, r.rt * kRows + row, mm, ll);
             }

@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             // (behind the barrier: of a single row tile, the run's last values may be the second group's, which has waited for their products)
             const bool nan = nans[run & (kTileSlots - 1)] != 0;
             ++run;
-            const float norm = cut ? 1.f : 1.f / l;
+            const float norm = l == 0.f ? 0.f : 1.f / l;
             mine_f *= norm; other_f *= norm;
             if (busy && (!single || X == 0)) {
 #pragma unroll 1

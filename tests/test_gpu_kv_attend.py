@@ -224,3 +224,13 @@ def test_scales_with_a_fraction_of_their_own(T, side, spread):
             if side in ("both", which):
                 t.mul_(torch.from_numpy(case.rs.uniform(1.0, 2.0, tuple(t.shape))).float().cuda())
         run(case, tensors=tensors, spread=spread)
+
+
+def test_largest_and_smallest_scales():
+    """Scales above 2^127 and below 2^-126 (values 0 and tiny codes where the scale is huge, so that outputs are finite)."""
+    for T in (1, 90):
+        case = _kv.Case([150, 40], [T - 1, T // 3], T, D=64, hq=4, hkv=2, seed=30 + T)
+        tensors = case.cache(spread=2.0 ** -7)
+        tensors[2].fill_(2.0 ** -127)
+        tensors[3].fill_(1.5 * 2.0 ** 127)
+        run(case, tensors=tensors)
