@@ -322,7 +322,8 @@ int opt_tree_kv_destroy(opt_tree_kv *kv);
  * for those that become subnormal) and the new ones are e4m3(x / s), rounded to nearest even.  Infinite inputs saturate and NaN stays
  * NaN; neither sets the scale.  The page's rows behind the step's last are left as they were.
  * Norm and rotation are computed in single precision and q_out is rounded once; where a scale or a code could come out otherwise than from the
- * exact value, that value is taken again in double precision. */
+ * exact value, or a norm's squares or products may pass single precision's range, that value is taken again in double precision.  (Keys beyond
+ * 448 * 2^127 saturate.) */
 int opt_tree_kv_append(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t layer, const opt_tree_kv_rows *q, const opt_tree_kv_rows *k,
                        const opt_tree_kv_rows *v, const opt_tree_kv_rows *q_out, const opt_tree_kv_step *step, const opt_tree_kv_turn *turn,
                        void *stream);

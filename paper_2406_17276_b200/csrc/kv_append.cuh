@@ -8,7 +8,7 @@
 // needs the largest value of a whole page and head before anything can be written, so one CTA takes a page of one head and one
 // side (keys or values), keeps what it has read in registers, and writes after one reduction: no atomics, nothing is read twice.
 // Queries have no such tie and are spread over further CTAs of the same launch, a warp for up to 16 heads (of 128 elements) of one token, so that
-// positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 114 us, for 4 x 4096 tokens of 32 / 8 heads of
+// positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 117 us, for 4 x 4096 tokens of 32 / 8 heads of
 // 128, normed and rotated; 54 us would be the bytes at 6.5 TB/s).  What bounds it now: a CTA's life is a chain of loads (lengths, rows and
 // table, angles, scale) around little work, and the arithmetic of norm, rotation and conversion takes 60 % of the issue slots.  Queries
 // alone take 59 us (4.6 TB/s), pages alone 52 us.
@@ -78,28 +78,45 @@ __device__ __forceinline__ void kv_angles(const KvAppend& a, int sub, int pos, K
         for (int i = 0; i < 8; ++i) g.s[i] = at < half ? -g.s[i] : g.s[i];
     }
 }
+// Largest magnitude; NaN if any is.
+__device__ __forceinline__ float max_abs8(const float (&x)[8]) {
+    float m = fabsf(x[0]);
+#pragma unroll
+    for (int i = 1; i < 7; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(x[i])), "f"(fabsf(x[i + 1])));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(x[7])));
+    return m;
+}
 // Norm and rotation with what does not depend on the row folded together, in packed pairs: x' = r (x (w c) + y (w_y s)), r the norm's factor.
+// true: weights so large that products may pass single precision's range on the way to a result within it.
 struct KvFold {
     unsigned long long c[4], s[4];
 };
 template <class T>
-__device__ __forceinline__ void kv_fold(const KvAppend& a, const uint16_t* weights, const KvAngles& g, int sub, int partner, KvFold& f) {
+__device__ __forceinline__ bool kv_fold(const KvAppend& a, const uint16_t* weights, const KvAngles& g, int sub, int partner, KvFold& f) {
     float c[8], s[8];
+    bool large = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) { c[i] = a.rot_dim ? g.c[i] : 1.f; s[i] = a.rot_dim ? g.s[i] : 0.f; }
     if (weights) {
         float w[8], y[8];
         unpack8<T>(load8(weights + sub * 8, a.wide_w), w);
+        large = max_abs8(w) > 0x1p60f;
         unpack8<T>(load8(weights + partner * 8, a.wide_w), y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) { c[i] *= w[i]; s[i] *= a.interleaved ? y[i ^ 1] : y[i]; }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f.c[i] = pack2(c[2 * i], c[2 * i + 1]); f.s[i] = pack2(s[2 * i], s[2 * i + 1]); }
+    return large;
 }
+// true: the norm's factor cannot be relied on, because the mean square is so large or small that squares or products may have passed single precision's
+// range (the same for all lanes of a row).  Such rows are taken again in double precision; that they may come costs 4 % of a call without any
+// (113 -> 117 us for the chunk above).
 template <int D, class T>
-__device__ __forceinline__ void turn_fast(const KvAppend& a, bool norm, const KvFold& f, int partner, uint4 raw, float (&out)[8]) {
+__device__ __forceinline__ bool turn_fast(const KvAppend& a, bool norm, const KvFold& f, int partner, uint4 raw, float (&out)[8]) {
     constexpr int kLanes = D / 8;
+    constexpr uint32_t kLeast = (127u - 40u) << 23, kMost = (127u + 100u) << 23;           // mean squares, as bits
+    bool wild = false;
     unsigned long long x[4];
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
@@ -114,7 +131,9 @@ __device__ __forceinline__ void turn_fast(const KvAppend& a, bool norm, const Kv
         float sum = lo + hi;
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        r = rsqrtf(sum * (1.f / D) + a.eps);
+        const float mean = sum * (1.f / D) + a.eps;
+        r = rsqrtf(mean);
+        wild = __float_as_uint(mean) - kLeast > kMost - kLeast;
     }
     const int lane = (threadIdx.x & 31 & ~(kLanes - 1)) + partner;
 #pragma unroll
@@ -135,9 +154,10 @@ __device__ __forceinline__ void turn_fast(const KvAppend& a, bool norm, const Kv
         if (norm) z = mul2(z, pack2(r, r));
         unpack2(z, out[2 * i], out[2 * i + 1]);
     }
+    return wild;
 }
-// The same of one row in double precision, for where the largest value lies so near a border of the scale that single precision could
-// take the other side.
+// The same of one row in double precision, for what single precision cannot be relied on: where the largest value lies so near a border of the
+// scale, or any so near the middle between two codes, that it could take the other side, and where squares, products or sums pass its range.
 template <int D, class T>
 __device__ __forceinline__ void turn_exact(const KvAppend& a, const uint16_t* weights, const KvAngles& g, int sub, int partner, uint4 raw, double (&x)[8]) {
     constexpr int kLanes = D / 8;
@@ -165,6 +185,12 @@ __device__ __forceinline__ void turn_exact(const KvAppend& a, const uint16_t* we
     for (int i = 0; i < 8; ++i) x[i] = x[i] * g.c[i] + y[i] * g.s[i];
 }
 
+// A double as the float that rounds to the same code or 16-bit number: cut off, with the last bit set if anything was.
+__device__ __forceinline__ float round_to_odd(double x) {
+    const float f = __double2float_rz(x);
+    return (double)f == x ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+
 // base: the sequence's base_pos, loaded by the caller together with its lengths (kv_base).
 __device__ __forceinline__ int kv_base(const KvAppend& a, int b) { return a.rot_dim && a.step.base_pos ? a.step.base_pos[b] : 0; }
 __device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int len, int base) {
@@ -176,6 +202,28 @@ __device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int 
         return pos < 0 ? 0 : a.positions - 1;
     }
     return pos;
+}
+
+// The groups of heads in the bits of `again`, in double precision.  A function of its own, so that it takes no registers where it is not called.
+template <int D, class T>
+__device__ __noinline__ void append_queries_again(const KvAppend& a, int b, int j, int h0, int pos, unsigned again) {
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+    const int sub = threadIdx.x & (kLanes - 1), partner = kv_partner(a, sub);
+    KvAngles g;
+    if (a.rot_dim) kv_angles(a, sub, pos, g);
+    while (again) {
+        const int h = h0 + (__ffs(again) - 1) * kRows;
+        again &= again - 1;
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (h < a.shape.q_heads) raw = load8(a.q.data + b * a.q.batch + j * a.q.token + h * a.q.head + sub * 8, a.wide_q);
+        double y[8];
+        turn_exact<D, T>(a, a.q_norm, g, sub, partner, raw, y);
+        if (h < a.shape.q_heads) {
+            const uint4 o = make_uint4(from_float2<T>(round_to_odd(y[0]), round_to_odd(y[1])), from_float2<T>(round_to_odd(y[2]), round_to_odd(y[3])),
+                                       from_float2<T>(round_to_odd(y[4]), round_to_odd(y[5])), from_float2<T>(round_to_odd(y[6]), round_to_odd(y[7])));
+            store8(const_cast<uint16_t*>(a.q_out.data) + b * a.q_out.batch + j * a.q_out.token + h * a.q_out.head + sub * 8, o, a.wide_out);
+        }
+    }
 }
 
 // The queries: a warp takes kAppendRows groups of heads of one token.
@@ -201,34 +249,33 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
     if (!kv_sequence(a.shape, a.step, b, len, tokens, a.status) || j >= tokens) return;
     KvAngles g;
     KvFold f;
-    const int partner = kv_partner(a, sub);
-    if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, j, len, base), g);
-    kv_fold<T>(a, a.q_norm, g, sub, partner, f);
+    const int partner = kv_partner(a, sub), pos = kv_position(a, b, j, len, base);
+    if (a.rot_dim) kv_angles(a, sub, pos, g);
+    const bool large = __any_sync(0xFFFFFFFFu, kv_fold<T>(a, a.q_norm, g, sub, partner, f));
+    unsigned again = 0;                                      // rows that single precision cannot be relied on for
 #pragma unroll
     for (int i = 0; i < kAppendRows; ++i) {
         if (part * kAppendRows * kRows + i * kRows >= (unsigned)a.shape.q_heads) break;    // the same for the whole warp
         float x[8];
-        turn_fast<D, T>(a, a.q_norm != nullptr, f, partner, raw[i], x);
-        if (h0 + i * kRows < a.shape.q_heads) {
+        const bool wild = turn_fast<D, T>(a, a.q_norm != nullptr, f, partner, raw[i], x) || large;
+        if (wild) again |= 1u << i;
+        if (!wild && h0 + i * kRows < a.shape.q_heads) {     // (rows that are taken again are read again, perhaps from where they are written to)
             const uint4 o = make_uint4(from_float2<T>(x[0], x[1]), from_float2<T>(x[2], x[3]), from_float2<T>(x[4], x[5]), from_float2<T>(x[6], x[7]));
             store8(to + (h0 + i * kRows) * a.q_out.head, o, a.wide_out);
         }
     }
+    if (!a.q_norm || !__any_sync(0xFFFFFFFFu, again != 0)) return;
+    again = __reduce_or_sync(0xFFFFFFFFu, again);
+    append_queries_again<D, T>(a, (int)b, j, h0, pos, again);
 }
 
 __device__ __forceinline__ float finite_abs(float x) {      // infinities saturate and NaN stays NaN: neither sets the scale
     const float m = fabsf(x);
-    return m <= 3.402823466e38f ? m : 0.f;
+    return m < INFINITY ? m : 0.f;
 }
 __device__ __forceinline__ double finite_abs(double x) {
     const double m = fabs(x);
-    return m <= 3.402823466e38 ? m : 0.0;
-}
-
-// A double as the float that rounds to the same code: cut off, with the last bit set if anything was.
-__device__ __forceinline__ float round_to_odd(double x) {
-    const float f = __double2float_rz(x);
-    return (double)f == x ? f : __uint_as_float(__float_as_uint(f) | 1u);
+    return m < (double)INFINITY ? m : 0.0;
 }
 
 // kPasses: row groups per warp that cover a page.
@@ -276,7 +323,8 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
     const int partner = kv_partner(a, sub);
 
     float x[kPasses][8];
-    float most = 0.f;
+    float most = 0.f;                                                        // an infinity: has to be found in double precision
+    unsigned again = 0;                                                      // passes of this warp that are taken again in double precision
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         if (turns && (i * kWarpsN + warp) * kRows < n) {                     // the same for the whole warp
@@ -285,23 +333,37 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
             KvFold f;
             if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len, base), g);
             kv_fold<T>(a, a.k_norm, g, sub, partner, f);
-            turn_fast<D, T>(a, a.k_norm != nullptr, f, partner, raw[i], x[i]);
+            const bool wild = turn_fast<D, T>(a, a.k_norm != nullptr, f, partner, raw[i], x[i]);
+            const float top = max_abs8(x[i]);
+            const bool doubt = (wild || !(top < INFINITY)) && r < n;
+            if (doubt) again |= 1u << i;
+            most = fmaxf(most, doubt ? INFINITY : top);
         } else {
             unpack8<T>(raw[i], x[i]);
+            const float top = max_abs8(x[i]);
+            if (top < INFINITY) {
+                most = fmaxf(most, top);
+            } else {
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t w = e < 2 ? raw[i].x : e < 4 ? raw[i].y : e < 6 ? raw[i].z : raw[i].w;
+                    const float2 two = to_float2<T>(w);
+                    most = fmaxf(most, finite_abs(e & 1 ? two.y : two.x));
+                }
+            }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_abs(x[i][e]));
     }
+    again = __reduce_or_sync(0xFFFFFFFFu, again);
     most = warp_max_f32(most);
     if (lane == 0) warp_max[warp] = __float_as_uint(most);
     __syncthreads();
 #pragma unroll
     for (int w1 = 0; w1 < kWarpsN; ++w1) most = fmaxf(most, __uint_as_float(warp_max[w1]));
-    // Single precision is off by less than 1e-6; nearer than 1e-5 to a border the largest value is found again in double
-    // precision, so that the scale, which is a whole power of two, does not hang on a rounding.
+    // Single precision is off by less than 1e-6; nearer than 1e-5 to a border, or where it cannot be relied on, the largest value is found again in
+    // double precision, so that the scale, which is a whole power of two, does not hang on a rounding.
     const uint32_t frac = __float_as_uint(most) & 0x7FFFFFu;
     int e = scale_exponent(__float_as_uint(most));
-    if (turns && frac > 0x600000u - 147u && frac < 0x600000u + 147u) {
+    if (turns && (most == INFINITY || (frac > 0x600000u - 147u && frac < 0x600000u + 147u))) {
         double exact = 0.0;
 #pragma unroll 1
         for (int i = 0; i < kPasses; ++i) {
@@ -323,7 +385,7 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
         for (int w1 = 0; w1 < kWarpsN; ++w1) all = warp_max64[w1] > all ? warp_max64[w1] : all;
         // 1.75 in the fraction of a double
         e = (int)(all >> 52) - 1023 - 8 + ((all & 0xFFFFFFFFFFFFFull) > 0xC000000000000ull ? 1 : 0);
-        e = e < kLeastScaleExp ? kLeastScaleExp : e;
+        e = e < kLeastScaleExp ? kLeastScaleExp : min(e, 127);
     }
     const float now = fmaxf(was, power_of_two(e)), inv = 1.f / now;
     if (older && now > was) {                                                // the page's older entries to the larger scale
@@ -335,7 +397,6 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
     // a norm).  Rows with a value that near the middle between two codes are taken again in double precision below, so that what is
     // stored is the rounding of the exact value.
     const float tol = (a.k_norm ? 1.2e-6f : 4e-7f) * inv;
-    unsigned again = 0;                                                      // passes of this warp
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int r = (i * kWarpsN + warp) * kRows + lane / kLanes;
@@ -369,9 +430,10 @@ __global__ void __launch_bounds__(kThreadsN, kThreadsN == 512 ? 1 : kThreadsN ==
         if (a.rot_dim) kv_angles(a, sub, kv_position(a, b, lo - len + min(r, n - 1), len, base), g);
         turn_exact<D, T>(a, a.k_norm, g, sub, partner, raw2, y);
         if (r < n) {
+            const double by = 1.0 / (double)now;
             uint2 o;
-            o.x = to_e4m3x4(round_to_odd(y[0]) * inv, round_to_odd(y[1]) * inv, round_to_odd(y[2]) * inv, round_to_odd(y[3]) * inv);
-            o.y = to_e4m3x4(round_to_odd(y[4]) * inv, round_to_odd(y[5]) * inv, round_to_odd(y[6]) * inv, round_to_odd(y[7]) * inv);
+            o.x = to_e4m3x4(round_to_odd(y[0] * by), round_to_odd(y[1] * by), round_to_odd(y[2] * by), round_to_odd(y[3] * by));
+            o.y = to_e4m3x4(round_to_odd(y[4] * by), round_to_odd(y[5] * by), round_to_odd(y[6] * by), round_to_odd(y[7] * by));
             *reinterpret_cast<uint2*>(codes + (long long)(lo - start + r) * D + sub * 8) = o;
         }
     }

@@ -186,3 +186,39 @@ def test_positions_and_pages_out_of_range_are_recorded():
         rest = torch.ones(case.num_pages, dtype=torch.bool, device="cuda")
         rest[other] = False
         assert torch.equal(now[0, rest], before[0, rest]) and not torch.equal(now, before)
+
+
+@pytest.mark.parametrize("D,page,rot,interleaved", [(64, 16, 64, False), (128, 32, 128, True), (128, 128, 0, False), (64, 64, 32, False)])
+def test_norms_of_the_whole_range_of_the_type(D, page, rot, interleaved):
+    """bf16 rows whose squares pass single precision's range at either end, beside ordinary ones: queries, scales and codes."""
+    for eps in (0.0, 1e-5):
+        case = _kv.Case([5, 0, page, 3], [6, 6, 6, 6], 7, hq=4, hkv=2, D=D, page=page, seed=D + page)
+        q, k, v = case.rows(4), case.rows(2), case.rows(2)
+        for t in (q, k):
+            t[0] *= 1e25
+            t[1] *= 1e-25
+            t[2, ::2] *= 1e-30
+            t[2, 1::2] *= 1e19
+            t[3, 2, 1, 3] = 3e38
+            t[3, 4, 0] = 3e38
+            t[3, 5, 1] *= 1e-10
+        _run(case, rot=rot, interleaved=interleaved, norm=True, eps=eps, rows=(q, k, v))
+
+
+def test_norm_weights_of_the_whole_range_of_the_type():
+    """Products that pass single precision's range on the way to an ordinary result, and keys beyond that range."""
+    case = _kv.Case([5, 0], [6, 6], 7, hq=4, hkv=2, D=64, seed=11)
+    q, k, v = case.rows(4, 1e15), case.rows(2, 1e15), case.rows(2)
+    kv, cache, cs = case.handle(binding), binding.KVCache(*case.cache()), case.cos_sin(64)
+    w = (1e30 * (1 + torch.rand(64, generator=torch.Generator().manual_seed(1)))).to(case.dtype).cuda()
+    codes, scale = _kv.f8(cache.k)[0], _kv.f64(cache.k_scale)[0]
+    got = kv.append(cache, 0, q, k, v, case.dev_step(binding), cos_sin=cs, q_norm=w, k_norm=w, eps=0.0)
+    turn = lambda x: np.stack([_kv.turned(_kv.f64(x)[b], _kv.f64(w), 0.0, _kv.f64(cs)[_kv.positions(case.step, b, 7)][:, None], 64, False) for b in range(2)])  # noqa: E731
+    want = turn(q)
+    assert (np.abs(_kv.f64(got) - want) <= np.abs(want) * 2.0 ** -8 + 2e-6 * np.abs(want).max(-1, keepdims=True)).all()
+    _kv.append(codes, scale, case.table, case.step, turn(k), case.page)
+    assert np.array_equal(_kv.f64(cache.k_scale)[0], scale) and np.array_equal(_kv.f8(cache.k)[0], codes)
+    # rotation alone, of values near the type's largest: pairs sum to more than single precision holds
+    case = _kv.Case([5, 0], [6, 6], 7, hq=4, hkv=2, D=64, seed=12)
+    k = (3.3e38 * torch.sign(case.rows(2).float())).to(case.dtype)
+    _run(case, rot=64, rows=(case.rows(4), k, case.rows(2)), with_q=False)
