@@ -41,7 +41,8 @@ struct KvAppend {
 constexpr int kAppendRows = 8;           // row groups a warp of a query CTA takes, all of one token: positions and angles are looked up once
 
 // A lane holds eight consecutive elements of a row, D / 8 consecutive lanes a row.  Rotation is x' = x c + y s with y the other element of
-// the pair, which another lane (`partner`) or this one holds, and the sign in s; elements that are not rotated have c = 1, s = 0.
+// the pair, which another lane (`partner`) or this one holds, and the sign in s; elements that are not rotated have c = 1, s = 0.  (An
+// infinity there makes NaN of that; rows with such a result are taken again without it.)
 struct KvAngles {
     float c[8], s[8];
 };
@@ -182,7 +183,7 @@ __device__ __forceinline__ void turn_exact(const KvAppend& a, const uint16_t* we
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = a.interleaved ? x[i ^ 1] : __shfl_sync(0xFFFFFFFFu, x[i], lane);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * g.c[i] + y[i] * g.s[i];
+    for (int i = 0; i < 8; ++i) x[i] = sub * 8 < a.rot_dim ? x[i] * g.c[i] + y[i] * g.s[i] : x[i];
 }
 
 // A double as the float that rounds to the same code or 16-bit number: cut off, with the last bit set if anything was.
@@ -252,19 +253,21 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
     const int partner = kv_partner(a, sub), pos = kv_position(a, b, j, len, base);
     if (a.rot_dim) kv_angles(a, sub, pos, g);
     const bool large = __any_sync(0xFFFFFFFFu, kv_fold<T>(a, a.q_norm, g, sub, partner, f));
+    const bool partly = a.rot_dim > 0 && a.rot_dim < D;
     unsigned again = 0;                                      // rows that single precision cannot be relied on for
 #pragma unroll
     for (int i = 0; i < kAppendRows; ++i) {
         if (part * kAppendRows * kRows + i * kRows >= (unsigned)a.shape.q_heads) break;    // the same for the whole warp
         float x[8];
-        const bool wild = turn_fast<D, T>(a, a.q_norm != nullptr, f, partner, raw[i], x) || large;
+        bool wild = turn_fast<D, T>(a, a.q_norm != nullptr, f, partner, raw[i], x) || large;
+        if (partly) wild = __any_sync(0xFFFFFFFFu, wild || !(max_abs8(x) < INFINITY));
         if (wild) again |= 1u << i;
         if (!wild && h0 + i * kRows < a.shape.q_heads) {     // (rows that are taken again are read again, perhaps from where they are written to)
             const uint4 o = make_uint4(from_float2<T>(x[0], x[1]), from_float2<T>(x[2], x[3]), from_float2<T>(x[4], x[5]), from_float2<T>(x[6], x[7]));
             store8(to + (h0 + i * kRows) * a.q_out.head, o, a.wide_out);
         }
     }
-    if (!a.q_norm || !__any_sync(0xFFFFFFFFu, again != 0)) return;
+    if ((!a.q_norm && !partly) || !__any_sync(0xFFFFFFFFu, again != 0)) return;
     again = __reduce_or_sync(0xFFFFFFFFu, again);
     append_queries_again<D, T>(a, (int)b, j, h0, pos, again);
 }

@@ -222,3 +222,19 @@ def test_norm_weights_of_the_whole_range_of_the_type():
     case = _kv.Case([5, 0], [6, 6], 7, hq=4, hkv=2, D=64, seed=12)
     k = (3.3e38 * torch.sign(case.rows(2).float())).to(case.dtype)
     _run(case, rot=64, rows=(case.rows(4), k, case.rows(2)), with_q=False)
+
+
+@pytest.mark.parametrize("rot,interleaved", [(16, False), (48, False), (16, True), (48, True)])
+@pytest.mark.parametrize("D,dtype", [(64, BF), (128, HF)])
+def test_infinities_and_nan_behind_the_rotated_part(rot, interleaved, D, dtype):
+    """Elements that are not rotated come through as they are, and do not reach their neighbours; rotated ones saturate."""
+    case = _kv.Case([3, 0], [3, 3], 4, hq=2, hkv=2, D=D, dtype=dtype, seed=rot + D)
+    q, k, v = (case.rows(2) for _ in range(3))
+    for t in (q, k):
+        t[0, 1, 0, rot + 3], t[0, 2, 1, rot + 7], t[0, 2, 1, D - 1] = float("inf"), float("-inf"), float("nan")
+        t[0, 3, 0, rot + 2] = float("inf")
+    k[0, 3, 0, 5] = float("inf")
+    kv, cache = case.handle(binding), binding.KVCache(*case.cache())
+    got = kv.append(cache, 0, q, k, v, case.dev_step(binding), cos_sin=case.cos_sin(rot), interleaved=interleaved)
+    assert np.array_equal(_kv.f64(got[..., rot:]), _kv.f64(q[..., rot:]), equal_nan=True) and torch.isfinite(got[..., :rot].float()).all()
+    _run(case, rot=rot, interleaved=interleaved, rows=(q, k, v), with_q=False)
