@@ -343,7 +343,7 @@ int opt_tree_kv_attend(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t 
 
 /* The accepted path's entries of all layers to the end of the prefix: slot kv_len + kv_gather[j] -> slot kv_len + j, j < kv_keep.
  *   kv_gather  (dev) [B][G], kv_keep (dev) [B]: as written by opt_tree_post_verify (G = max_depth + 1 <= 1024); strictly ascending
- *   new_len    (dev) [B] or NULL, not kv_len itself: kv_len + kv_keep, the next step's kv_len
+ *   new_len    (dev) [B] or NULL, in none of what kv_len, kv_gather and kv_keep occupy: kv_len + kv_keep, the next step's kv_len
  * A page that takes entries whose scale is larger than its own is brought to the largest of them, all its rows.  A sequence with
  * entries out of order or out of range is left as it is (new_len = kv_len, OPT_TREE_ERR_INTERNAL in the status word); kv_keep 0: nothing moves. */
 int opt_tree_kv_compact(opt_tree_kv *kv, const opt_tree_kv_cache *cache, const int32_t *kv_len, const int32_t *kv_gather,

@@ -55,6 +55,10 @@ ot::KvRows rows_of(const opt_tree_kv_rows* r) {
     return ot::KvRows{static_cast<const uint16_t*>(r->data), (long long)r->batch, (long long)r->token, (long long)r->head};
 }
 bool bad_rows(const opt_tree_kv_rows* r) { return !r || !r->data || (reinterpret_cast<uintptr_t>(r->data) & 1u); }
+bool overlap(const int32_t* a, size_t n, const int32_t* b, size_t m) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + m * sizeof(int32_t) && y < x + n * sizeof(int32_t);
+}
 int wide(const opt_tree_kv_rows* r) {
     return ((reinterpret_cast<uintptr_t>(r->data) & 15u) == 0 && r->batch % 8 == 0 && r->token % 8 == 0 && r->head % 8 == 0) ? 1 : 0;
 }
@@ -262,9 +266,10 @@ int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
 
 int opt_tree_kv_compact(opt_tree_kv* kv, const opt_tree_kv_cache* cache, const int32_t* kv_len, const int32_t* kv_gather, const int32_t* kv_keep,
                         int32_t G, int32_t B, int32_t* new_len, void* stream) {
-    if (!kv || bad_cache(cache) || !kv_len || !kv_gather || !kv_keep || G < 1 || B < 1 || B > kv->cfg.max_batch || new_len == kv_len)
-        return OPT_TREE_ERR_INVALID_ARG;
+    if (!kv || bad_cache(cache) || !kv_len || !kv_gather || !kv_keep || G < 1 || B < 1 || B > kv->cfg.max_batch) return OPT_TREE_ERR_INVALID_ARG;
     if (G > ot::kCompactMost) return OPT_TREE_ERR_UNSUPPORTED;
+    // (layer 0 writes the new lengths while the others may still read)
+    if (new_len && (overlap(new_len, B, kv_len, B) || overlap(new_len, B, kv_keep, B) || overlap(new_len, B, kv_gather, (size_t)B * G))) return OPT_TREE_ERR_INVALID_ARG;
     if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
     ot::KvCompact a{kv->shape, cache->k, cache->v, cache->k_scale, cache->v_scale, cache->block_table, kv_len, kv_gather, kv_keep, G, new_len, kv->status};
     launch_after(kv->cfg.head_dim == 64 ? ot::kv_compact_kernel<64> : ot::kv_compact_kernel<128>, dim3(B, kv->cfg.layers), dim3(ot::kCompactThreads), 0,

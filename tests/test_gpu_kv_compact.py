@@ -73,3 +73,19 @@ def test_indices_out_of_order_or_range_leave_the_sequence():
         new = kv.compact(binding.KVCache(*case.cache()), torch.tensor([4, 9], dtype=torch.int32, device="cuda"),
                          torch.tensor([[0, 1, 2], [0, 1, 2]], dtype=torch.int32, device="cuda"), torch.tensor([keep, 1], dtype=torch.int32, device="cuda"))
         assert kv.device_status() == binding.ERR_INTERNAL and new.tolist() == [4, 10]
+
+
+def test_new_lengths_that_overlap_what_is_read_are_refused():
+    """All layers read the lengths, counts and indices while the first one writes the new lengths."""
+    case = _kv.Case([4, 9, 7], [12, 12, 12], 13, layers=3, seed=4)
+    kv, cache = case.handle(binding), binding.KVCache(*case.cache())
+    ints = torch.tensor([0, 0, 0, 4, 9, 7, 2, 3, 1, 0, 3, 5, 0, 4, 6, 0, 2, 7, 0, 0, 0], dtype=torch.int32, device="cuda")
+    lens, keep, gather = ints[3:6], ints[6:9], ints[9:18].view(3, 3)
+    before = ints.clone()
+    for at in (1, 2, 3, 4, 6, 8, 9, 12, 17):
+        with pytest.raises(binding.OptTreeError):
+            kv.compact(cache, lens, gather, keep, new_len=ints[at:at + 3])
+    assert kv.launch_count() == 0 and torch.equal(ints, before)
+    for at in (0, 18):                                         # next to them is fine
+        assert kv.compact(cache, lens, gather, keep, new_len=ints[at:at + 3]).tolist() == [6, 12, 8]
+    assert kv.device_status() == 0
