@@ -32,8 +32,8 @@ bool supported_cfg(const opt_tree_kv_config* c) {
     if (c->head_dim != 64 && c->head_dim != 128) return false;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return false;
     if (c->max_batch > 32767 || c->layers > 32767 || c->q_heads > 32767) return false;
-    if ((long long)c->max_pages * c->page > 1ll << 30) return false;                                   // slots of a sequence
-    if ((long long)c->max_batch * c->max_step * c->q_heads > 0x7FFFFFFFll) return false;               // rows of a step
+    if ((long long)c->max_pages * c->page > 1ll << 30 || c->max_step > 1 << 30) return false;         // slots of a sequence, of which a step's tokens take some
+    if ((long long)c->max_batch * c->max_step * c->q_heads > 0x7FFFFFFFll - 512) return false;         // rows of a step, with a tile's padding
     const long long touched = (c->max_step + c->page - 2) / c->page + 1;
     if ((long long)c->max_batch * touched * c->kv_heads * 2 > 0x3FFFFFFFll) return false;              // CTAs of an append
     return true;

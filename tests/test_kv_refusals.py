@@ -66,3 +66,13 @@ def test_cache_tensors_are_looked_at():
     for B, T in ((3, 6), (2, 7), (2, 70)):
         with pytest.raises(ValueError):
             step.c_struct(B, T, torch.device("cpu"))
+
+
+@pytest.mark.parametrize("change", [dict(q_heads=1, kv_heads=1, max_batch=1, max_step=(1 << 31) - 1), dict(q_heads=1, kv_heads=1, max_batch=1, max_step=(1 << 30) + 1),
+                                    dict(q_heads=32767, kv_heads=1, max_batch=1, max_step=65538), dict(q_heads=2, kv_heads=2, max_batch=1, max_step=(1 << 30) - 1)])
+def test_sizes_whose_sums_pass_31_bits(L, change):
+    """Steps longer than any sequence, and rows that with a tile's padding no longer count in 31 bits."""
+    cfg = binding.KVConfig(**{**GOOD, **change})
+    kv = C.c_void_p(1)
+    assert L.opt_tree_kv_workspace_bytes(cfg) == 0
+    assert L.opt_tree_kv_create(C.byref(kv), cfg) == binding.ERR_UNSUPPORTED and not kv
