@@ -275,6 +275,8 @@ int opt_tree_step_host(opt_tree_ctx *ctx, const void *draft_logits_bf16, const v
  *            contiguous; any base a 16-bit element may have, fastest where base and strides are multiples of 16 bytes.
  * Tokens beyond a sequence's nodes + 1 are padding: their rows are not used and not written anywhere.
  *
+ * Every pointer lies on a boundary of its elements (OPT_TREE_ERR_INVALID_ARG otherwise).
+ *
  * A handle owns a workspace and a status word only and belongs to the device that was current at its creation; calls are made
  * with that device current (otherwise OPT_TREE_ERR_INVALID_ARG).  The calls only enqueue work on `stream`, may be captured into
  * graphs, and never allocate or synchronise.  Calls on one handle share its workspace: those that may run at the same time (two

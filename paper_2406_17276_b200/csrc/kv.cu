@@ -43,18 +43,21 @@ bool on_device(const opt_tree_kv* kv) {
     int dev = -1;
     return cudaGetDevice(&dev) == cudaSuccess && dev == kv->device;
 }
+// Whether an address is off a boundary (loads from there would fault).
+bool off(const void* p, uintptr_t boundary) { return (reinterpret_cast<uintptr_t>(p) & (boundary - 1)) != 0; }
 bool bad_cache(const opt_tree_kv_cache* c) {
     if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->block_table) return true;
-    return ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) != 0;
+    return off(c->k, 16) || off(c->v, 16) || off(c->k_scale, 4) || off(c->v_scale, 4) || off(c->block_table, 4);
 }
 bool bad_step(const opt_tree_kv* kv, const opt_tree_kv_step* s) {
-    return !s || s->B < 1 || s->B > kv->cfg.max_batch || s->T < 1 || s->T > kv->cfg.max_step || !s->kv_len;
+    return !s || s->B < 1 || s->B > kv->cfg.max_batch || s->T < 1 || s->T > kv->cfg.max_step || !s->kv_len || off(s->kv_len, 4) || off(s->nodes, 4) ||
+           off(s->base_pos, 4) || off(s->position_ids, 4) || off(s->mask, 8);
 }
 ot::KvStep step_of(const opt_tree_kv_step* s) { return ot::KvStep{s->B, s->T, s->kv_len, s->nodes, s->base_pos, s->position_ids, s->mask}; }
 ot::KvRows rows_of(const opt_tree_kv_rows* r) {
     return ot::KvRows{static_cast<const uint16_t*>(r->data), (long long)r->batch, (long long)r->token, (long long)r->head};
 }
-bool bad_rows(const opt_tree_kv_rows* r) { return !r || !r->data || (reinterpret_cast<uintptr_t>(r->data) & 1u); }
+bool bad_rows(const opt_tree_kv_rows* r) { return !r || !r->data || off(r->data, 2); }
 bool overlap(const int32_t* a, size_t n, const int32_t* b, size_t m) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + m * sizeof(int32_t) && y < x + n * sizeof(int32_t);
@@ -186,8 +189,7 @@ int opt_tree_kv_append(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
     if (!turn) turn = &none;
     const int D = kv->cfg.head_dim;
     if (turn->rot_dim < 0 || turn->rot_dim > D || turn->rot_dim % 16 || (turn->rot_dim && (!turn->cos_sin || turn->positions < 1)) ||
-        ((turn->q_norm || turn->k_norm) && !(turn->eps >= 0.f)) || ((reinterpret_cast<uintptr_t>(turn->cos_sin) & 3u) != 0) ||
-        (((reinterpret_cast<uintptr_t>(turn->q_norm) | reinterpret_cast<uintptr_t>(turn->k_norm)) & 1u) != 0))
+        ((turn->q_norm || turn->k_norm) && !(turn->eps >= 0.f)) || off(turn->cos_sin, 4) || off(turn->q_norm, 2) || off(turn->k_norm, 2))
         return OPT_TREE_ERR_INVALID_ARG;
     if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
     ot::KvAppend a;
@@ -228,7 +230,7 @@ int opt_tree_kv_append(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
 int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t layer, const opt_tree_kv_rows* q, const opt_tree_kv_step* step,
                        float scale, const opt_tree_kv_rows* out, float* lse, void* stream) {
     if (!kv || bad_cache(cache) || layer < 0 || layer >= kv->cfg.layers || bad_rows(q) || bad_rows(out) || bad_step(kv, step) || !(scale > 0.f) ||
-        scale > 1e38f)
+        scale > 1e38f || off(lse, 4))
         return OPT_TREE_ERR_INVALID_ARG;
     if (!on_device(kv)) return OPT_TREE_ERR_INVALID_ARG;
     ot::KvAttend a;
@@ -266,7 +268,9 @@ int opt_tree_kv_attend(opt_tree_kv* kv, const opt_tree_kv_cache* cache, int32_t 
 
 int opt_tree_kv_compact(opt_tree_kv* kv, const opt_tree_kv_cache* cache, const int32_t* kv_len, const int32_t* kv_gather, const int32_t* kv_keep,
                         int32_t G, int32_t B, int32_t* new_len, void* stream) {
-    if (!kv || bad_cache(cache) || !kv_len || !kv_gather || !kv_keep || G < 1 || B < 1 || B > kv->cfg.max_batch) return OPT_TREE_ERR_INVALID_ARG;
+    if (!kv || bad_cache(cache) || !kv_len || !kv_gather || !kv_keep || G < 1 || B < 1 || B > kv->cfg.max_batch || off(kv_len, 4) || off(kv_gather, 4) ||
+        off(kv_keep, 4) || off(new_len, 4))
+        return OPT_TREE_ERR_INVALID_ARG;
     if (G > ot::kCompactMost) return OPT_TREE_ERR_UNSUPPORTED;
     // (layer 0 writes the new lengths while the others may still read)
     if (new_len && (overlap(new_len, B, kv_len, B) || overlap(new_len, B, kv_keep, B) || overlap(new_len, B, kv_gather, (size_t)B * G))) return OPT_TREE_ERR_INVALID_ARG;

@@ -243,3 +243,35 @@ def test_calls_too_large_to_count_are_refused():
     cache, rows, step = struct.pack("@5P", *[some] * 5), struct.pack("@P3q", some, 0, 0, 0), struct.pack("@2i5P", 4096, 1, some, 0, 0, 0, 0)
     assert L.opt_tree_kv_attend(kv, cache, 0, rows, step, 1.0, rows, None, None) == binding.ERR_UNSUPPORTED
     assert L.opt_tree_kv_launch_count(kv) == 0 and L.opt_tree_kv_destroy(kv) == binding.OK
+
+
+def test_pointers_off_their_elements_boundary_are_refused():
+    """Scales, tables, lengths, masks and sums that do not lie on a boundary of their elements would fault in a kernel."""
+    case, tensors, rows = _problem(2, 5, True, 14, hq=4, hkv=2, D=64)
+    kv, t = case.handle(binding), tensors
+    step = case.dev_step(binding)
+    L, h = binding.lib(), kv._kv
+    p = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
+    good_cache, good_step = [p(x) for x in t], [p(x) for x in (step.kv_len, step.nodes, step.base_pos, step.position_ids, step.mask)]
+    packed = [struct.pack("@P3q", p(x), *x.stride()[:3]) for x in rows]
+    lse, keep, gather, new = (torch.zeros(64, dtype=torch.float32, device="cuda") for _ in range(4))
+
+    def attend(cache, st, sums):
+        return L.opt_tree_kv_attend(h, struct.pack("@5P", *cache), 0, packed[0], struct.pack("@2i5P", 2, 5, *st), 1.0, packed[0], sums, None)
+
+    def append(cache, st):
+        return L.opt_tree_kv_append(h, struct.pack("@5P", *cache), 0, None, packed[1], packed[2], None, struct.pack("@2i5P", 2, 5, *st), None, None)
+
+    def compact(cache, *ints):
+        return L.opt_tree_kv_compact(h, struct.pack("@5P", *cache), *ints[:3], 3, 2, ints[3], None)
+    ints = [p(step.kv_len), p(gather), p(keep), p(new)]
+    for i in range(5):
+        for by in (1, 2):
+            bad = [x + by * (k == i) for k, x in enumerate(good_cache)]
+            assert attend(bad, good_step, None) == append(bad, good_step) == compact(bad, *ints) == binding.ERR_INVALID_ARG
+            bad = [x + (4 if i == 4 else by) * (k == i) for k, x in enumerate(good_step)]
+            assert attend(good_cache, bad, None) == append(good_cache, bad) == binding.ERR_INVALID_ARG
+    assert attend(good_cache, good_step, p(lse) + 2) == binding.ERR_INVALID_ARG
+    for i in range(4):
+        assert compact(good_cache, *[x + 2 * (k == i) for k, x in enumerate(ints)]) == binding.ERR_INVALID_ARG
+    assert kv.launch_count() == 0 and kv.device_status() == 0
