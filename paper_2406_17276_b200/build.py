@@ -12,7 +12,7 @@ OBJECTS = os.path.join(_HERE, "_build")
 # Each source with its own flags (the tree kernels are all held to 80 registers, the cache kernels state theirs themselves) and the
 # headers it includes.
 TREE_HEADERS = ["common.cuh", "launch.cuh", "pipeline.cuh", "row_topk.cuh", "select.cuh"]
-KV_HEADERS = ["common.cuh", "launch.cuh", "kv_common.cuh", "kv_append.cuh", "kv_attend.cuh", "kv_attend_few.cuh", "kv_attend_tiles.cuh", "kv_compact.cuh"]
+KV_HEADERS = ["common.cuh", "copy_ring.cuh", "launch.cuh", "kv_common.cuh", "kv_append.cuh", "kv_attend.cuh", "kv_attend_few.cuh", "kv_attend_tiles.cuh", "kv_compact.cuh"]
 SOURCES = [("opt_tree.cu", ["-maxrregcount=80"], TREE_HEADERS), ("kv.cu", [], KV_HEADERS)]
 NVCC = "/usr/local/cuda/bin/nvcc"
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]

@@ -12,6 +12,7 @@
 
 #include <type_traits>
 
+#include "copy_ring.cuh"
 #include "kv_attend.cuh"
 
 namespace ot {
@@ -42,6 +43,7 @@ template <int D, int NT> struct FewLayout {
 template <int D, int NT, class T>
 __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::kPerSm) kv_attend_few_kernel(const __grid_constant__ KvAttend a) {
     using L = FewLayout<D, NT>;
+    using Ring = CopyRing<L::kStages>;
     constexpr int kRows = L::kRows, kStages = L::kStages, kKeys = L::kKeys, kChunks = D / 64, kSteps = D / 16, kVWords = D / 32;
     extern __shared__ __align__(128) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -98,8 +100,8 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
         id[1] = blocks > 32 ? look(1) : -1;
         auto fetch = [&](int i, int page_id) {               // lane 0: block i of this run into its stage
             const uint32_t at = count + i;
-            unsigned char* stage = ring + at % kStages * L::kStage;
-            unsigned long long* bar = bars + at % kStages;
+            unsigned char* stage = ring + Ring::stage(at) * L::kStage;
+            unsigned long long* bar = bars + Ring::stage(at);
             const long long row = ((long long)page_id * a.shape.kv_heads + r.h) * a.shape.page + ((key0 + i * L::kKeys) & (a.shape.page - 1));
             mbar_expect_tx(bar, 32 * D);
             bulk_load(stage, a.kc + row * D, 16 * D, bar);
@@ -164,8 +166,11 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
             const int ahead = i + kStages;
             const int p = (ahead >> 5) == (i >> 5) ? __shfl_sync(0xFFFFFFFFu, id[0], ahead & 31) : __shfl_sync(0xFFFFFFFFu, id[1], ahead & 31);
             const uint32_t at = count + i;
-            const unsigned char* stage = ring + at % kStages * L::kStage;
-            if (!dead && !mbar_wait_warp(bars + at % kStages, at / kStages & 1, a.status)) dead = true;
+            const unsigned char* stage = ring + Ring::stage(at) * L::kStage;
+            if (!dead && !mbar_wait_warp(bars + Ring::stage(at), Ring::parity(at), a.status)) {
+                dead = true;                                 // what is in flight lands before anything else uses the ring
+                Ring::drain(at, count + min(blocks, i + kStages), [&](uint32_t st, uint32_t parity) { mbar_wait_warp(bars + st, parity, a.status); });
+            }
             const int s0 = key0 + i * L::kKeys;              // first slot of the block
             // scores: rows x keys, key 4 (n >> 1) + 2 half + (n & 1) as column n of each half
             float s[2][4];
@@ -268,9 +273,6 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
             }
             __syncwarp();                                    // the stage has been read by all lanes
             if (lane == 0 && ahead < blocks && !dead) fetch(ahead, p);
-        }
-        if (dead) {                                          // what is in flight lands before anything else uses the ring
-            for (int s = 0; s < kStages; ++s) mbar_wait_warp(bars + s, (count + blocks - 1 - s) / kStages & 1, a.status, 1 << 20);
         }
         count += blocks;
         __syncthreads();                                     // every warp is done with its ring: the parts go over it

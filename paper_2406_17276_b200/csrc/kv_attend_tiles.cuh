@@ -25,6 +25,7 @@
 
 #include <type_traits>
 
+#include "copy_ring.cuh"
 #include "kv_attend.cuh"
 
 namespace ot {
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
     tc_fence_after();
     const uint32_t tmem = words[0];
     grid_dependency_wait();
-    // A wait that runs out is recorded; this warp waits for nothing more then and leaves at the end of its run (softmax: of all runs).
+    // A wait that runs out is recorded; this warp waits for nothing more then and leaves at the end of its run (softmax: of all runs; conversion: at once).
     bool dead = false;
     auto wait = [&](int bar, uint32_t parity) { dead = dead || !mbar_wait_warp(bars + bar, parity, a.status); };
     KvRun r;
@@ -562,6 +563,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bars + raw_free + st);
                     wait(free_ + stage, phase ^ 1);
+                    if (dead) break;                         // (no stage is handed back any more, so the copying warp gets no further ahead)
 #pragma unroll
                     for (int i = 0; i < kIter; ++i) {
                         const int row = i * kAtOnce + key;
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
     if (warp == 17) {
         // ---- copies: pages of a key tile, a lane for each 16 keys; four tiles are looked up at a time, four ahead ----
-        uint32_t done = 0;
+        uint32_t done = 0, issued_k = 0, issued_v = 0;       // key tiles, and those of which keys and values were copied
         int run = 0;
         const int shift = a.shape.page_shift, inside = a.shape.page - 1;
         const int copy_rows = min(a.shape.page, kTileKeys);
@@ -665,11 +667,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
                 if (lane == 0) mbar_expect_tx(bars + L::kBarRKFull + st, bytes);
                 __syncwarp();
                 if (copies) bulk_load(smem + L::kRawK + st * L::kCodes + lane * 16 * D, a.kc + row * D, copy_rows * D, bars + L::kBarRKFull + st);
+                ++issued_k;
                 wait(L::kBarRVFree + st, phase ^ 1);
                 if (dead) continue;
                 if (lane == 0) mbar_expect_tx(bars + L::kBarRVFull + st, bytes);
                 __syncwarp();
                 if (copies) bulk_load(smem + L::kRawV + st * L::kCodes + lane * 16 * D, a.vc + row * D, copy_rows * D, bars + L::kBarRVFull + st);
+                ++issued_v;
             }
             ++run;
         }
@@ -679,11 +683,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             a.cuts[blockIdx.x] = before;
         }
         // copies in flight land before the CTA ends, also where their reader has given up
-        for (uint32_t i = 0; i < L::kRaw; ++i)
-            if (dead && done > i) {
-                mbar_wait_warp(bars + L::kBarRKFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
-                mbar_wait_warp(bars + L::kBarRVFull + (done - 1 - i) % L::kRaw, (done - 1 - i) / L::kRaw & 1, a.status, 1 << 20);
-            }
+        using Ring = CopyRing<L::kRaw>;
+        Ring::drain(Ring::oldest(issued_k), issued_k, [&](uint32_t st, uint32_t parity) { mbar_wait_warp(bars + L::kBarRKFull + st, parity, a.status); });
+        Ring::drain(Ring::oldest(issued_v), issued_v, [&](uint32_t st, uint32_t parity) { mbar_wait_warp(bars + L::kBarRVFull + st, parity, a.status); });
     } else if (warp == 16) {
         // ---- products: one lane issues ----
         if (elect_one()) {
