@@ -38,3 +38,16 @@ def test_host_only_entry_points_work_without_a_gpu():
     assert L.opt_tree_workspace_bytes(binding.Config(32000, 4096, 1024, 10, 511, 32)) == 0      # more layers than a mailbox item can name
     assert L.opt_tree_workspace_bytes(binding.Config(32000, 4096, 64, 33, 10, 32)) == 0
     assert L.opt_tree_workspace_bytes(None) == 0
+
+
+def test_a_source_is_compiled_again_when_any_header_it_includes_is_newer(tmp_path, monkeypatch):
+    """What a source depends on is read from its includes, headers of headers among them; every header belongs to a source."""
+    found = {name: {os.path.basename(d) for d in build.dependencies(os.path.join(build.CSRC, name))} for name, *_ in build.SOURCES}
+    assert {"kv.cu", "kv_append.cuh", "kv_attend.cuh", "kv_common.cuh", "common.cuh", "copy_ring.cuh", "opt_tree.h"} <= found["kv.cu"]
+    assert "pipeline.cuh" in found["opt_tree.cu"] and "kv_attend.cuh" not in found["opt_tree.cu"]
+    assert {f for f in os.listdir(build.CSRC) if not f.startswith(".")} <= set().union(*found.values())
+    # a header that nothing has been told about
+    (tmp_path / "a.cu").write_text('#include <vector>\n#include "b.cuh"\n')
+    (tmp_path / "b.cuh").write_text('  # include "c.cuh"\n#include "b.cuh"\n')
+    (tmp_path / "c.cuh").write_text("")
+    assert {os.path.basename(d) for d in build.dependencies(str(tmp_path / "a.cu"))} == {"a.cu", "b.cuh", "c.cuh"}
