@@ -325,6 +325,7 @@ if torch.cuda.is_available():            # the same without the wrappers' checks
     _current_device = getattr(torch._C, "_cuda_getDevice", _current_device)
     _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
 
+_grad_enabled = torch.is_grad_enabled
 _ROW_TYPES = {torch.bfloat16: 0, torch.float16: 1}
 _F8, _F32, _I32, _I64 = torch.float8_e4m3fn, torch.float32, torch.int32, torch.int64
 
@@ -336,6 +337,11 @@ def _index(device: torch.device) -> int:
 
 # The structures of opt_tree_kv_* as bytes: packed faster than ctypes fills a Structure, and handed over by their address.
 _CACHE, _STEP, _ROWS, _TURN = (struct.Struct(f).pack for f in ("@5P", "@2i5P", "@P3q", "@P3iPPf"))
+
+
+def _no_gradients(t, name: str):
+    if t is not None and t.requires_grad and _grad_enabled():
+        raise ValueError(f"{name}: asks for gradients, which the cache operators do not have; call them under torch.no_grad() or detach it")
 
 
 def _addr(t, name: str, dtype, shape, index: int):
@@ -385,7 +391,8 @@ class KVStep:
 
 
 class TreeKV:
-    """A handle of the cache operators (opt_tree_kv_*): fixed sizes, workspace allocated once, on one device."""
+    """A handle of the cache operators (opt_tree_kv_*): fixed sizes, workspace allocated once, on one device.  For serving: there is no backward
+    pass, and inputs that ask for gradients are refused."""
 
     def __init__(self, q_heads: int, kv_heads: int, head_dim: int, page: int, num_pages: int, max_pages: int, max_batch: int, max_step: int,
                  layers: int = 1, dtype: torch.dtype = torch.bfloat16, device: str | torch.device | None = None):
@@ -429,6 +436,8 @@ class TreeKV:
         return KVCache(k, v, ks, vs, block_table)
 
     def _rows(self, t: torch.Tensor, name: str, shape) -> bytes:
+        if t.requires_grad:
+            _no_gradients(t, name)
         st = t.stride()
         if t.dtype is self.dtype and t.shape == shape and t.get_device() == self._at and st[3] == 1:
             return _ROWS(t.data_ptr(), st[0], st[1], st[2])
@@ -464,6 +473,7 @@ class TreeKV:
             if q_out is None:
                 q_out = torch.empty(shape, dtype=self.dtype, device=self.device)
             qr, qo = rows(q, "q", shape), rows(q_out, "q_out", shape)
+        _no_gradients(cos_sin, "cos_sin"), _no_gradients(q_norm, "q_norm"), _no_gradients(k_norm, "k_norm")
         angles, positions, rot = 0, 0, 0
         if cos_sin is not None:
             positions, rot = cos_sin.shape

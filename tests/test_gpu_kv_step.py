@@ -275,3 +275,26 @@ def test_pointers_off_their_elements_boundary_are_refused():
     for i in range(4):
         assert compact(good_cache, *[x + 2 * (k == i) for k, x in enumerate(ints)]) == binding.ERR_INVALID_ARG
     assert kv.launch_count() == 0 and kv.device_status() == 0
+
+
+def test_inputs_that_ask_for_gradients_are_refused():
+    """There is no backward pass: outputs would come without the gradients that were asked for."""
+    case, tensors, rows = _problem(2, 5, True, 15, hq=4, hkv=2, D=64)
+    kv, cache, step, cs = case.handle(binding), binding.KVCache(*tensors), case.dev_step(binding), case.cos_sin(64)
+    w = torch.ones(64, dtype=case.dtype, device="cuda")
+    asked = lambda t: t.clone().requires_grad_()  # noqa: E731
+    q, k, v = rows
+    calls = [lambda: kv.attend(cache, 0, asked(q), step), lambda: kv.attend(cache, 0, q, step, out=asked(q) * 1)]
+    for i in range(3):
+        calls.append(lambda i=i: kv.append(cache, 0, *[asked(t) if j == i else t for j, t in enumerate(rows)], step, cos_sin=cs))
+    for name in ("q_norm", "k_norm"):
+        calls.append(lambda name=name: kv.append(cache, 0, q, k, v, step, cos_sin=cs, **{name: asked(w)}))
+    calls.append(lambda: kv.append(cache, 0, q, k, v, step, cos_sin=asked(cs)))
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert kv.launch_count() == 0
+    with torch.no_grad():                                      # parameters of a model that serves
+        for call in calls:
+            call()
+    assert kv.launch_count() >= len(calls) and kv.device_status() == 0
