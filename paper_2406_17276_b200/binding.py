@@ -380,9 +380,7 @@ class KVStep:
         self.kv_len, self.nodes, self.base_pos, self.position_ids, self.mask = kv_len, nodes, base_pos, position_ids, mask
 
     def c_struct(self, B: int, T: int, device: torch.device) -> bytes:
-        return self._pack(B, T, _index(device))
-
-    def _pack(self, B: int, T: int, index: int) -> bytes:
+        index = _index(device)
         one, nodes, base, pos, mask = (B,), self.nodes, self.base_pos, self.position_ids, self.mask
         return _STEP(B, T, _addr(self.kv_len, "kv_len", _I32, one, index), 0 if nodes is None else _addr(nodes, "nodes", _I32, one, index),
                      0 if base is None else _addr(base, "base_pos", _I32, one, index),
@@ -480,7 +478,7 @@ class TreeKV:
             angles = _addr(cos_sin, "cos_sin", _F32, (positions, rot), at)
         turn = _TURN(angles, positions, rot, 1 if interleaved else 0, 0 if q_norm is None else _addr(q_norm, "q_norm", self.dtype, (D,), at),
                      0 if k_norm is None else _addr(k_norm, "k_norm", self.dtype, (D,), at), eps)
-        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, rows(k, "k", each), rows(v, "v", each), qo, step._pack(B, T, at), turn)
+        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, rows(k, "k", each), rows(v, "v", each), qo, step.c_struct(B, T, self.device), turn)
         return q_out
 
     def attend(self, cache: KVCache, layer: int, q: torch.Tensor, step: KVStep, scale: float | None = None, out: torch.Tensor | None = None,
@@ -491,7 +489,7 @@ class TreeKV:
         shape = (B, T, heads, self._D)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, self._rows(q, "q", shape), step._pack(B, T, at), self._scale if scale is None else scale,
+        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, self._rows(q, "q", shape), step.c_struct(B, T, self.device), self._scale if scale is None else scale,
                    self._rows(out, "out", shape), None if lse is None else _addr(lse, "lse", _F32, (B, T, heads), at))
         return out
 
