@@ -258,7 +258,8 @@ int opt_tree_step_host(opt_tree_ctx *ctx, const void *draft_logits_bf16, const v
  *
  *   cache    k, v (dev) [layers][num_pages][kv_heads][page][head_dim] e4m3 codes, 16-byte aligned, and
  *            k_scale, v_scale (dev) [layers][num_pages][kv_heads] float: an entry stands for code * scale.  opt_tree_kv_append and
- *            opt_tree_kv_compact write powers of two; opt_tree_kv_attend takes any positive finite scale.
+ *            opt_tree_kv_compact write powers of two, and are exact as said below for pages that hold such; opt_tree_kv_attend takes any
+ *            positive finite scale.
  *            block_table (dev) [B][max_pages] int32: slot s of sequence b (its s-th cached token) is row s % page of page
  *            block_table[b][s / page].  Entries beyond a sequence's last slot are not read.  Sequences may share pages that lie wholly below
  *            their kv_len; a page that takes a step's tokens belongs to one sequence and stands once in its table.
@@ -333,8 +334,11 @@ int opt_tree_kv_append(opt_tree_kv *kv, const opt_tree_kv_cache *cache, int32_t 
 /* out_i = sum_j softmax_j(scale * q_i . k_j) v_j over the slots that token i of the step sees, whose keys and values are in layer `layer`
  * of the cache (the step's own included: append first).  Products are taken in half precision, in which e4m3 codes are exact, and summed in
  * single precision, as are softmax sums; probabilities are rounded to half precision (2^-11 of each at most).  Pages are brought to a
- * common scale for that: values keep all their bits where their page's scale is at least 2^-15 of the largest among the slots that are read
- * together, and 2^-25 of that largest below.  Rows that see a NaN are NaN (in the elements of a value that is NaN), others are not.
+ * common power of two for that: keys and values keep all their bits where their page's scale is at least 2^-15 of the largest among the slots that are
+ * read together, and 2^-25 of that largest below.  What a scale is over its power of two is multiplied in in single precision.  bf16 queries are
+ * half-precision numbers from 2^-17 to 2^15: smaller elements are rounded by up to 2^-25 in rows whose largest lies between 2^-6 and 2^15; other rows are
+ * scaled by a power of two of their own, which rounds elements below 2^-25 of the row's largest.  Scores have to stay within single precision's range.
+ * Rows that see a NaN are NaN (in the elements of a value that is NaN), others are not.
  * Work is divided by what there is to read, whatever the lengths; results do not depend on how calls before or beside it went, but their
  * last bits may depend on the other sequences of the batch, which decide where a sequence is cut.
  * B * kv_heads * (row tiles of T) * (key tiles of max_pages * page) may not pass 2^30 (OPT_TREE_ERR_UNSUPPORTED).

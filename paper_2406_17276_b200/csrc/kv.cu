@@ -93,7 +93,9 @@ template <int D, class T> AttendVariant attend_variant(int rows, bool brief) {
 }
 // The kernel for `rows` query rows per sequence and key head at most.  brief: with 16 rows at a time an SM has no more than two key tiles
 // to do even if every page is full; up to 64 rows that is quicker than the tensor cores' tiles, which take longer to start (16.4 us
-// against 20.7 for 44 rows over 900 slots, 8 key heads; over 8000 slots 35.6 against 31.3).
+// against 20.7 for 44 rows over 900 slots, 8 key heads; over 8000 slots 35.6 against 31.3).  It goes by what a block table can hold, since only the
+// device knows the lengths: short contexts under wide tables take the tiles (the same 44 rows: 16.4 us under a table of 57 pages of 16, 20.9 under one
+// of 256).
 AttendVariant attend_for(const opt_tree_kv_config& c, int rows, bool brief) {
     const bool bf16 = c.dtype == OPT_TREE_BF16;
     if (c.head_dim == 64) return bf16 ? attend_variant<64, __nv_bfloat16>(rows, brief) : attend_variant<64, __half>(rows, brief);

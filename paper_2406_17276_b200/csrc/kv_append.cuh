@@ -10,8 +10,8 @@
 // Queries have no such tie and are spread over further CTAs of the same launch, a warp for up to 16 heads (of 128 elements) of one token, so that
 // positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 117 us, for 4 x 4096 tokens of 32 / 8 heads of
 // 128, normed and rotated; 54 us would be the bytes at 6.5 TB/s).  What bounds it now: a CTA's life is a chain of loads (lengths, rows and
-// table, angles, scale) around little work, and the arithmetic of norm, rotation and conversion takes 60 % of the issue slots.  Queries
-// alone take 59 us (4.6 TB/s), pages alone 52 us.
+// table, angles, scale) around little work, and the arithmetic of norm, rotation and conversion takes 58 % of the issue slots.  Pages
+// alone (a call without queries) take 67 us of the 117.
 
 #pragma once
 

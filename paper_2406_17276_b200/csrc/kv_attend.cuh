@@ -5,8 +5,8 @@
 // All query rows of a sequence that read one key head (tokens x query heads per key head, token-major) are taken together, so that
 // a page is read and converted once for them.  Work is cut by the clock and not by sequence: the tiles (sequence, key head, row
 // tile, tile of keys) are numbered in that order and every CTA takes an equal run of them, whatever the lengths; a row tile that is cut
-// leaves its parts (maximum, sum, output) in the workspace, and the CTA that finishes last joins them in order, so
-// results do not depend on who that is.
+// leaves its parts (maximum, sum, output) in the workspace.  Few rows: the CTA that finishes last joins them; many rows: a kernel of its own does.
+// Either joins them in the order of the keys, so results do not depend on who finishes when.
 #pragma once
 
 #include "kv_common.cuh"

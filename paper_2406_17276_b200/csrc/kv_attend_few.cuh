@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(FewLayout<D, NT>::kThreads, FewLayout<D, NT>::
         const int key0 = (r.k0 * L::kWarps + warp) * 16;
         const int blocks = key0 < r.keys ? min(r.k1 - r.k0, (r.keys - key0 + L::kKeys - 1) / L::kKeys) : 0;
         // queries: rows g and g + 8, elements in the order in which the lanes hold keys.  bf16 rows are brought to half precision by
-        // a power of two of their own (exact but for elements below 2^-22 of the row's largest)
+        // a power of two of their own (exact but for elements below 2^-25 of the row's largest)
         uint4 raw[NT][kChunks * 2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {

@@ -8,7 +8,7 @@
 // per 256 rows.  (Eight-bit operands would need queries and probabilities in two parts each: the same tensor time as half precision, and
 // twice the conversions per row.)
 // What bounds it: the chain of a key tile (codes, conversion, scores, exponentials, values), no unit by itself.  32 trees of 65 tokens over up to 4096
-// slots, 32 / 8 heads of 128: 197 us, 470 TFLOP/s; the exponentials alone would take 40 us, the products 56.
+// slots, 32 / 8 heads of 128: 201 us, 464 TFLOP/s; the exponentials alone would take 40 us, the products 56.
 //
 // Roles: warps 0-3 and 4-7 softmax, one thread a row; warps 8-11 convert keys, 12-15 values; warp 16 issues the products; warp 17 divides the
 // work, looks pages up and copies their codes into shared memory a key tile ahead; two warps fill the last warpgroup.  Barriers (all waits bounded;
@@ -280,8 +280,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tiles_kernel(const 
             const bool mine = in_tile < rows, busy = (warp & 3) * 32 < rows;       // this thread, this warp
             const int token = (int)a.by_group.div((unsigned)min(row, r.tokens * a.group - 1));
             // Queries to shared memory, D / 8 lanes a row, all of a warp's 32 rows in flight.  bf16 numbers from 2^-17 on to 2^15 are half-precision
-            // numbers too; where a row is larger, or has nothing above 2^-6, the warp's rows are brought there by powers of two of
-            // their own (exact but for elements below 2^-22 of the row's largest).
+            // numbers too, and smaller ones are rounded by up to 2^-25 (2^-19 of the row's largest at most): rows whose largest lies between 2^-6 and 2^15
+            // are taken as they are, which spares a second pass over them.  Where a row is larger or smaller, the warp's
+            // rows are brought there by powers of two of their own (exact but for elements below 2^-25 of the row's largest).
             float qf = a.scale;
             {
                 constexpr int kRowLanes = D / 8, kAt = 32 / kRowLanes, kLoads = 32 / kAt;
