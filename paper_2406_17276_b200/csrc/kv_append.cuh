@@ -205,21 +205,22 @@ __device__ __forceinline__ int kv_position(const KvAppend& a, int b, int j, int 
     return pos;
 }
 
-// The groups of heads in the bits of `again`, in double precision.  A function of its own, so that it takes no registers where it is not called.
+// The rows in the bits of `mine` (one bit a group of heads, the same for the lanes of a row), in double precision.  Other rows of the group have been
+// written, perhaps to where they came from.  A function of its own, so that it takes no registers where it is not called.
 template <int D, class T>
-__device__ __noinline__ void append_queries_again(const KvAppend& a, int b, int j, int h0, int pos, unsigned again) {
+__device__ __noinline__ void append_queries_again(const KvAppend& a, int b, int j, int h0, int pos, unsigned mine) {
     constexpr int kLanes = D / 8, kRows = 32 / kLanes;
     const int sub = threadIdx.x & (kLanes - 1), partner = kv_partner(a, sub);
     KvAngles g;
     if (a.rot_dim) kv_angles(a, sub, pos, g);
-    while (again) {
-        const int h = h0 + (__ffs(again) - 1) * kRows;
-        again &= again - 1;
+    for (unsigned again = __reduce_or_sync(0xFFFFFFFFu, mine); again; again &= again - 1) {
+        const int i = __ffs(again) - 1, h = h0 + i * kRows;
+        const bool on = (mine >> i & 1) && h < a.shape.q_heads;
         uint4 raw = make_uint4(0, 0, 0, 0);
-        if (h < a.shape.q_heads) raw = load8(a.q.data + b * a.q.batch + j * a.q.token + h * a.q.head + sub * 8, a.wide_q);
+        if (on) raw = load8(a.q.data + b * a.q.batch + j * a.q.token + h * a.q.head + sub * 8, a.wide_q);
         double y[8];
         turn_exact<D, T>(a, a.q_norm, g, sub, partner, raw, y);
-        if (h < a.shape.q_heads) {
+        if (on) {
             const uint4 o = make_uint4(from_float2<T>(round_to_odd(y[0]), round_to_odd(y[1])), from_float2<T>(round_to_odd(y[2]), round_to_odd(y[3])),
                                        from_float2<T>(round_to_odd(y[4]), round_to_odd(y[5])), from_float2<T>(round_to_odd(y[6]), round_to_odd(y[7])));
             store8(const_cast<uint16_t*>(a.q_out.data) + b * a.q_out.batch + j * a.q_out.token + h * a.q_out.head + sub * 8, o, a.wide_out);
@@ -254,7 +255,7 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
     if (a.rot_dim) kv_angles(a, sub, pos, g);
     const bool large = __any_sync(0xFFFFFFFFu, kv_fold<T>(a, a.q_norm, g, sub, partner, f));
     const bool partly = a.rot_dim > 0 && a.rot_dim < D;
-    unsigned again = 0;                                      // rows that single precision cannot be relied on for
+    unsigned again = 0;                                      // this lane's rows that single precision cannot be relied on for
 #pragma unroll
     for (int i = 0; i < kAppendRows; ++i) {
         if (part * kAppendRows * kRows + i * kRows >= (unsigned)a.shape.q_heads) break;    // the same for the whole warp
@@ -268,7 +269,6 @@ __device__ __forceinline__ void append_queries(const KvAppend& a, unsigned block
         }
     }
     if ((!a.q_norm && !partly) || !__any_sync(0xFFFFFFFFu, again != 0)) return;
-    again = __reduce_or_sync(0xFFFFFFFFu, again);
     append_queries_again<D, T>(a, (int)b, j, h0, pos, again);
 }
 

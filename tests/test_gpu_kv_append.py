@@ -238,3 +238,19 @@ def test_infinities_and_nan_behind_the_rotated_part(rot, interleaved, D, dtype):
     got = kv.append(cache, 0, q, k, v, case.dev_step(binding), cos_sin=case.cos_sin(rot), interleaved=interleaved)
     assert np.array_equal(_kv.f64(got[..., rot:]), _kv.f64(q[..., rot:]), equal_nan=True) and torch.isfinite(got[..., :rot].float()).all()
     _run(case, rot=rot, interleaved=interleaved, rows=(q, k, v), with_q=False)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rot", [None, 32])
+def test_queries_in_place_beside_rows_that_are_taken_again(D, rot):
+    """Rows of 1e25 between ordinary ones of the same token: in place as apart."""
+    case = _kv.Case([4, 9], [4, 4], 5, hq=10, hkv=2, D=D, seed=D)
+    kv, cache = case.handle(binding), binding.KVCache(*case.cache())
+    q, k, v = case.rows(10), case.rows(2), case.rows(2)
+    for h in (0, 3, 6, 9):
+        q[:, h % 5, h] *= 1e25
+    w = (1 + 0.3 * torch.from_numpy(case.rs.standard_normal(D))).to(case.dtype).cuda()
+    more = dict(cos_sin=case.cos_sin(rot or D), q_norm=w, k_norm=w)
+    apart = kv.append(cache, 0, q, k, v, case.dev_step(binding), q_out=torch.zeros_like(q), **more)
+    kv.append(cache, 0, q, k, v, case.dev_step(binding), q_out=q, **more)
+    assert torch.equal(apart, q) and apart.float().abs().max() < 100
