@@ -339,8 +339,8 @@ def _index(device: torch.device) -> int:
 _CACHE, _STEP, _ROWS, _TURN = (struct.Struct(f).pack for f in ("@5P", "@2i5P", "@P3q", "@P3iPPf"))
 
 
-def _no_gradients(t, name: str):
-    if t is not None and t.requires_grad and _grad_enabled():
+def _no_gradients(name: str):
+    if _grad_enabled():
         raise ValueError(f"{name}: asks for gradients, which the cache operators do not have; call them under torch.no_grad() or detach it")
 
 
@@ -379,8 +379,8 @@ class KVStep:
                  position_ids: torch.Tensor | None = None, mask: torch.Tensor | None = None):
         self.kv_len, self.nodes, self.base_pos, self.position_ids, self.mask = kv_len, nodes, base_pos, position_ids, mask
 
-    def c_struct(self, B: int, T: int, device: torch.device) -> bytes:
-        index = _index(device)
+    def c_struct(self, B: int, T: int, device: torch.device | int) -> bytes:
+        index = device if type(device) is int else _index(device)
         one, nodes, base, pos, mask = (B,), self.nodes, self.base_pos, self.position_ids, self.mask
         return _STEP(B, T, _addr(self.kv_len, "kv_len", _I32, one, index), 0 if nodes is None else _addr(nodes, "nodes", _I32, one, index),
                      0 if base is None else _addr(base, "base_pos", _I32, one, index),
@@ -435,11 +435,16 @@ class TreeKV:
 
     def _rows(self, t: torch.Tensor, name: str, shape) -> bytes:
         if t.requires_grad:
-            _no_gradients(t, name)
+            _no_gradients(name)
         st = t.stride()
         if t.dtype is self.dtype and t.shape == shape and t.get_device() == self._at and st[3] == 1:
             return _ROWS(t.data_ptr(), st[0], st[1], st[2])
         raise ValueError(f"{name}: {self.dtype} {tuple(shape)} with contiguous rows on {self.device} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def _weight(self, t: torch.Tensor, name: str) -> int:
+        if t.requires_grad:
+            _no_gradients(name)
+        return _addr(t, name, self.dtype, (self._D,), self._at)
 
     def _cache(self, cache: KVCache, B: int) -> bytes:
         table = cache.table_shape
@@ -471,14 +476,15 @@ class TreeKV:
             if q_out is None:
                 q_out = torch.empty(shape, dtype=self.dtype, device=self.device)
             qr, qo = rows(q, "q", shape), rows(q_out, "q_out", shape)
-        _no_gradients(cos_sin, "cos_sin"), _no_gradients(q_norm, "q_norm"), _no_gradients(k_norm, "k_norm")
         angles, positions, rot = 0, 0, 0
         if cos_sin is not None:
             positions, rot = cos_sin.shape
+            if cos_sin.requires_grad:
+                _no_gradients("cos_sin")
             angles = _addr(cos_sin, "cos_sin", _F32, (positions, rot), at)
-        turn = _TURN(angles, positions, rot, 1 if interleaved else 0, 0 if q_norm is None else _addr(q_norm, "q_norm", self.dtype, (D,), at),
-                     0 if k_norm is None else _addr(k_norm, "k_norm", self.dtype, (D,), at), eps)
-        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, rows(k, "k", each), rows(v, "v", each), qo, step.c_struct(B, T, self.device), turn)
+        turn = _TURN(angles, positions, rot, 1 if interleaved else 0, 0 if q_norm is None else self._weight(q_norm, "q_norm"),
+                     0 if k_norm is None else self._weight(k_norm, "k_norm"), eps)
+        self._call("opt_tree_kv_append", self._cache(cache, B), layer, qr, rows(k, "k", each), rows(v, "v", each), qo, step.c_struct(B, T, at), turn)
         return q_out
 
     def attend(self, cache: KVCache, layer: int, q: torch.Tensor, step: KVStep, scale: float | None = None, out: torch.Tensor | None = None,
@@ -489,7 +495,7 @@ class TreeKV:
         shape = (B, T, heads, self._D)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, self._rows(q, "q", shape), step.c_struct(B, T, self.device), self._scale if scale is None else scale,
+        self._call("opt_tree_kv_attend", self._cache(cache, B), layer, self._rows(q, "q", shape), step.c_struct(B, T, at), self._scale if scale is None else scale,
                    self._rows(out, "out", shape), None if lse is None else _addr(lse, "lse", _F32, (B, T, heads), at))
         return out
 
