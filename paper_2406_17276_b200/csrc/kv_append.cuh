@@ -8,10 +8,10 @@
 // needs the largest value of a whole page and head before anything can be written, so one CTA takes a page of one head and one
 // side (keys or values), keeps what it has read in registers, and writes after one reduction: no atomics, nothing is read twice.
 // Queries have no such tie and are spread over further CTAs of the same launch, a warp for up to 16 heads (of 128 elements) of one token, so that
-// positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 117 us, for 4 x 4096 tokens of 32 / 8 heads of
+// positions, angles and weights are looked up and folded once (a row at a time: 211 us, now 118 us, for 4 x 4096 tokens of 32 / 8 heads of
 // 128, normed and rotated; 54 us would be the bytes at 6.5 TB/s).  What bounds it now: a CTA's life is a chain of loads (lengths, rows and
 // table, angles, scale) around little work, and the arithmetic of norm, rotation and conversion takes 58 % of the issue slots.  Pages
-// alone (a call without queries) take 67 us of the 117.
+// alone (a call without queries) take 67 us of the 118.
 
 #pragma once
 
@@ -111,8 +111,8 @@ __device__ __forceinline__ bool kv_fold(const KvAppend& a, const uint16_t* weigh
     return large;
 }
 // true: the norm's factor cannot be relied on, because the mean square is so large or small that squares or products may have passed single precision's
-// range (the same for all lanes of a row).  Such rows are taken again in double precision; that they may come costs 4 % of a call without any
-// (113 -> 117 us for the chunk above).
+// range (the same for all lanes of a row).  Such rows are taken again in double precision; that they may come costs 5 % of a call without any
+// (112 -> 118 us for the chunk above).
 template <int D, class T>
 __device__ __forceinline__ bool turn_fast(const KvAppend& a, bool norm, const KvFold& f, int partner, uint4 raw, float (&out)[8]) {
     constexpr int kLanes = D / 8;
